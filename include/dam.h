@@ -16,6 +16,9 @@
  *                             only the kept K/V rows.
  *   dam_kv_evict_plan, dam_kv_compact, dam_kv_remap_lists   drop the cached keys no future row of a
  *                             pattern mask attends and decode from the compacted cache (paper Sec. 2).
+ *   dam_kv_quantize, dam_kv_dequantize   K / V rows into a cache of 8-bit codes as they are made, and
+ *                             back; dam_sparse_attn_decode_quantized, _grouped_quantized,
+ *                             _patterns_quantized: the decodes over such a cache.
  *
  * Conventions shared by every entry point
  *   - Plain C. "device" pointers are HIP device addresses, "host" pointers are ordinary host memory.
@@ -516,6 +519,88 @@ int dam_kv_compact(const dam_evict_params *params, const int32_t *window, const 
 int dam_kv_remap_lists(const dam_evict_params *params, const int32_t *window, const int32_t *col_ptr,
                        const int32_t *cols, const int32_t *kept_ptr, const int32_t *kept_idx,
                        int32_t *kept_slot, void *stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * The KV cache in 8 bits: dam_kv_quantize, dam_kv_dequantize and the decodes over it
+ *
+ * A cache holds one code of 8 bits per element, and every `block` consecutive rows of a (sequence, KV head) share one
+ * scale byte s for K and one for V. A code c stands for c * 2^(s - 127), and for 0 where s is 0 (the library writes 0 and
+ * 1 to 249). Codes: DAM_KV_E4M3, 4 exponent bits with bias 7, 3 mantissa bits, no infinities, largest value 448; DAM_KV_INT8,
+ * two's complement, -127 to 127. A row that held a value that is not finite is stored as NaN throughout (e4m3 0x7F, int8
+ * -128 in every place): it takes no part in the scale of its block and reads as NaN, alone among its block's rows. A row
+ * whose first code is NaN is a NaN row; the library writes no others with such codes.
+ * Every value is a bf16 number, so the rows read back in bf16 or fp32 are the cache's values without another rounding.
+ * ---------------------------------------------------------------------------------------------- */
+typedef enum { DAM_KV_E4M3 = 0, DAM_KV_INT8 = 1 } dam_kv_format;
+
+/* kcache, vcache  device [batch][hkv][kv_capacity][head_dim] bytes, strides in the call's parameters, head_dim contiguous,
+ *                 rows and bases 16-byte aligned.
+ * kscale, vscale  device u8 [batch][hkv][ceil(kv_capacity / block)] by scale_stride, the blocks of a head contiguous. */
+typedef struct {
+  void *kcache, *vcache;
+  uint8_t *kscale, *vscale;
+  int32_t format;          /* dam_kv_format                                                          */
+  int32_t block;           /* rows that share a scale: 16, 32, 64 or 128                             */
+  int64_t scale_stride[2]; /* of the batch and KV head index                                         */
+} dam_quant_cache;
+
+typedef struct {
+  int32_t batch, hkv;
+  int32_t kv_capacity;  /* rows per (sequence, KV head) of the cache                                 */
+  int32_t head_dim;     /* 64 or 128                                                                 */
+  int32_t dtype;        /* dam_dtype of k and v                                                      */
+  int32_t n_rows;       /* rows per sequence in k and v; 0: nothing is done                          */
+  int32_t pos;          /* position of the first one where `start` is NULL                           */
+  int64_t k_stride[3];  /* element strides of batch, KV head and row of k and v; head_dim            */
+  int64_t v_stride[3];  /*   contiguous, rows and bases 16-byte aligned                              */
+  int64_t kv_stride[3]; /* element strides of batch, KV head and row of both caches                  */
+} dam_quant_params;
+
+/* Writes rows r = 0 .. count[b] - 1 of k and v to positions start[b] + r of sequence b.
+ * For K and V and every block of rows that new ones fall into, with a the largest magnitude of its new finite rows:
+ *     need = the smallest s >= 1 with a <= c_max * 2^(s - 127)   (c_max 448 or 127; need = 0 if a = 0)
+ *     s    = need where the block holds no row in front of start[b], else max(need, the block's scale so far)
+ *     code = x * 2^(127 - s) rounded to nearest, ties to even;  the rows in front: code * 2^(s_old - s), the same way
+ *            (where that would stand for 2^128 or more, no fp32 number any longer: the largest code below).
+ * Rows in front are positions below start[b]; codes at and behind start[b] + count[b] belong to no row, are left as they
+ * are and have to be written again before they are read. So a sequence is written front to back (each call continues where
+ * the last one ended, or goes back to any earlier position and drops what lies behind), and the result depends on where
+ * the calls' borders fall only inside the blocks that hold one.
+ * k, v     device [batch][hkv][n_rows][head_dim] by the strides.
+ * start    device i32 [batch] or NULL (pos for all); count device i32 [batch] or NULL (n_rows for all; counts above n_rows
+ *          or below 0 are taken as those). Device data that the host cannot check: a sequence whose start lies outside
+ *          [0, kv_capacity) has nothing written, rows that would lie behind the cache's end are dropped. With both NULL
+ *          pos + n_rows must not exceed kv_capacity (DAM_ERR_INVALID_ARG).
+ * No two calls may write the same block at the same time. */
+int dam_kv_quantize(const dam_quant_params *params, const dam_quant_cache *cache, const void *k, const void *v,
+                    const int32_t *start, const int32_t *count, void *stream);
+
+/* The values of rows start[b] + r, r = 0 .. count[b] - 1, into rows r of k and v (device, by the strides); the other rows of
+ * k and v are left as they are. Everything else as above. */
+int dam_kv_dequantize(const dam_quant_params *params, const dam_quant_cache *cache, const int32_t *start,
+                      const int32_t *count, void *k, void *v, void *stream);
+
+/* dam_sparse_attn_decode, _grouped and _patterns over such a cache: the same lists, plans, parameters (dtype is that of q and
+ * out, bf16 or fp32; kv_stride and kv_capacity are the cache's, its rows 16-byte aligned) and results, on the cache's values.
+ * Products and softmax are evaluated in fp32; where the products run on the matrix cores (bf16, head_dim 128, merged
+ * lists and plans) the values are exact bf16 numbers and the softmax weights go in as two bf16 terms each (16 bits).
+ * A NaN row makes the outputs of the heads that keep it NaN and no others. Plans are decoded for every dtype and head_dim.
+ * max_kept, the lists' bounds, clamped indices and empty lists (O = 0, lse = -inf) as for those calls. */
+size_t dam_sparse_attn_decode_quantized_workspace(const dam_decode_params *params, int64_t max_kept);
+int dam_sparse_attn_decode_quantized(const dam_decode_params *params, const void *q, const dam_quant_cache *cache,
+                                     const int32_t *kept_ptr, const int32_t *kept_idx, int64_t max_kept, void *out,
+                                     float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* The workspace of the two forms below (plans: with shared_lists = 1 and max_kept = max_entries). */
+size_t dam_sparse_attn_decode_grouped_quantized_workspace(const dam_decode_params *params, int64_t max_kept);
+int dam_sparse_attn_decode_grouped_quantized(const dam_decode_params *params, const void *q, const dam_quant_cache *cache,
+                                             const int32_t *kept_ptr, const int32_t *kept_idx, const uint8_t *kept_member,
+                                             int64_t max_kept, void *out, float *lse, void *ws, size_t ws_bytes,
+                                             void *stream);
+int dam_sparse_attn_decode_patterns_quantized(const dam_decode_params *params, const void *q, const dam_quant_cache *cache,
+                                              const int32_t *plan_ptr, const int32_t *plan_val, const uint8_t *plan_member,
+                                              const uint8_t *plan_table, int32_t n_flags, int32_t pos, int64_t max_entries,
+                                              void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------
  * Measurement helpers (no passage of the paper: they measure the chip's own ceilings, printed by the

@@ -26,6 +26,7 @@ DAM_MASK_GATHER_COLUMNS = 2
 DAM_MASK_GROUP_LISTS = 4
 DAM_MASK_PATTERN_PLAN = 8
 DAM_ATTN_RUNNING_REFERENCE = 1
+DAM_KV_E4M3, DAM_KV_INT8 = 0, 1
 TRANSFORMS = {"boxcox": 0, "raw_sum": 1, "average": 2, "log": 3, "yeo_johnson": 4, "zscore": 5, "minmax": 6,
               "sqrt": 7, "arcsinh": 8}
 
@@ -92,12 +93,27 @@ class EvictParams(ctypes.Structure):
                 ("kv_stride", ctypes.c_int64 * 3), ("compact_stride", ctypes.c_int64 * 3)]
 
 
+class QuantCacheView(ctypes.Structure):
+    _fields_ = [("kcache", ctypes.c_void_p), ("vcache", ctypes.c_void_p), ("kscale", ctypes.c_void_p),
+                ("vscale", ctypes.c_void_p), ("format", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("scale_stride", ctypes.c_int64 * 2)]
+
+
+class QuantParams(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("hkv", ctypes.c_int32), ("kv_capacity", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("pos", ctypes.c_int32),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3)]
+
+
 EXPORTS = ["dam_gather_stride", "dam_kv_evict_workspace", "dam_kv_evict_plan", "dam_kv_compact", "dam_kv_remap_lists", "dam_mask_build_workspace", "dam_mask_build", "dam_capture_workspace", "dam_capture_accumulate",
            "dam_mask_build_from_qk_workspace", "dam_mask_build_from_qk", "dam_sparse_attn_prefill_workspace",
            "dam_sparse_attn_prefill", "dam_sparse_attn_decode_workspace", "dam_sparse_attn_decode",
            "dam_sparse_attn_decode_grouped_workspace", "dam_sparse_attn_decode_grouped",
            "dam_sparse_attn_decode_patterns", "dam_sparse_attn_decode_grouped_static_limit", "dam_sparse_attn_decode_grouped_static", "dam_probe_mfma",
-           "dam_probe_stream_read", "dam_probe_row_lists", "dam_version"]
+           "dam_probe_stream_read", "dam_probe_row_lists", "dam_version", "dam_kv_quantize", "dam_kv_dequantize",
+           "dam_sparse_attn_decode_quantized_workspace", "dam_sparse_attn_decode_quantized",
+           "dam_sparse_attn_decode_grouped_quantized_workspace", "dam_sparse_attn_decode_grouped_quantized",
+           "dam_sparse_attn_decode_patterns_quantized"]
 
 _lib = None
 
@@ -156,6 +172,22 @@ def lib() -> ctypes.CDLL:
         L.dam_kv_compact.argtypes = [ctypes.POINTER(EvictParams), vp, vp, vp, vp, vp, vp, vp, vp]
         L.dam_kv_remap_lists.restype = ctypes.c_int
         L.dam_kv_remap_lists.argtypes = [ctypes.POINTER(EvictParams), vp, vp, vp, vp, vp, vp, vp]
+        QC, QP, DP = ctypes.POINTER(QuantCacheView), ctypes.POINTER(QuantParams), ctypes.POINTER(DecodeParams)
+        L.dam_kv_quantize.restype = ctypes.c_int
+        L.dam_kv_quantize.argtypes = [QP, QC, vp, vp, vp, vp, vp]
+        L.dam_kv_dequantize.restype = ctypes.c_int
+        L.dam_kv_dequantize.argtypes = [QP, QC, vp, vp, vp, vp, vp]
+        L.dam_sparse_attn_decode_quantized_workspace.restype = sz
+        L.dam_sparse_attn_decode_quantized_workspace.argtypes = [DP, i64]
+        L.dam_sparse_attn_decode_quantized.restype = ctypes.c_int
+        L.dam_sparse_attn_decode_quantized.argtypes = [DP, vp, QC, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.dam_sparse_attn_decode_grouped_quantized_workspace.restype = sz
+        L.dam_sparse_attn_decode_grouped_quantized_workspace.argtypes = [DP, i64]
+        L.dam_sparse_attn_decode_grouped_quantized.restype = ctypes.c_int
+        L.dam_sparse_attn_decode_grouped_quantized.argtypes = [DP, vp, QC, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.dam_sparse_attn_decode_patterns_quantized.restype = ctypes.c_int
+        L.dam_sparse_attn_decode_patterns_quantized.argtypes = [DP, vp, QC, vp, vp, vp, vp, ctypes.c_int32, ctypes.c_int32, i64,
+                                                                vp, vp, vp, sz, vp]
         L.dam_probe_mfma.restype = ctypes.c_int
         L.dam_probe_mfma.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, vp]
         L.dam_probe_stream_read.restype = ctypes.c_int
@@ -198,6 +230,7 @@ def _check(fn: str, st: int):
     if st == -1000:                # codes of _dam_native for what is no status of the library
         raise DamError("dtype", DAM_ERR_UNSUPPORTED)
     assert st != -1001, f"{fn}: shapes or strides of the tensors do not fit together"
+    assert st != -1002, f"{fn}: a tensor is not on the current device"
     raise DamError(fn, st)
 
 
@@ -578,6 +611,105 @@ def kv_remap_lists(plan: EvictionPlan, kept_ptr: torch.Tensor, kept_idx: torch.T
                                   _p(kept_idx), _p(out), _stream())
     _check("dam_kv_remap_lists", st)
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+@dataclass
+class QuantCache:
+    """A KV cache of 8-bit codes: k, v [B][Hkv][cap][d] (torch.float8_e4m3fn or torch.int8, identical strides, d contiguous),
+    kscale, vscale u8 [B][Hkv][ceil(cap / block)]: a code c of row r stands for c * 2^(scale[r // block] - 127)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    kscale: torch.Tensor
+    vscale: torch.Tensor
+    block: int
+
+def quant_cache(batch: int, hkv: int, capacity: int, head_dim: int, dtype=torch.float8_e4m3fn, block: int = 64,
+                device="cuda") -> QuantCache:
+    """An empty cache: allocation only."""
+    codes = [torch.zeros((batch, hkv, capacity, head_dim), dtype=torch.uint8, device=device).view(dtype) for _ in range(2)]
+    scales = [torch.zeros((batch, hkv, (capacity + block - 1) // block), dtype=torch.uint8, device=device) for _ in range(2)]
+    return QuantCache(*codes, *scales, block)
+
+
+def dam_kv_quantize(cache: QuantCache, k, v, pos: int = 0, start=None, count=None) -> None:
+    """Rows k, v [B][Hkv][n][d] (bf16 or fp32, d contiguous) to positions pos .. pos + n - 1 of every sequence, or the first
+    count[b] of them to start[b] .. (i32 [B] on the device)."""
+    st = (_native or native()).kv_rows(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, k, v, pos, start, count, True)
+    if st:
+        _check("dam_kv_quantize", st)
+
+
+def dam_kv_dequantize(cache: QuantCache, k=None, v=None, pos: int = 0, start=None, count=None, rows: int = 0,
+                      dtype=torch.bfloat16):
+    """The cache's values of the same rows into k, v [B][Hkv][n][d]; the rows behind count[b] are left as they are (zero in
+    tensors made here: n = rows, dtype)."""
+    if k is None:
+        k = torch.zeros((*cache.k.shape[:2], rows, cache.k.shape[3]), dtype=dtype, device=cache.k.device)
+    if v is None:
+        v = torch.zeros_like(k)
+    st = (_native or native()).kv_rows(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, k, v, pos, start, count, False)
+    if st:
+        _check("dam_kv_dequantize", st)
+    return k, v
+
+
+def decode_quantized_workspace(q, cache: QuantCache, max_kept: int, grouped: bool, shared_lists: bool = False) -> torch.Tensor:
+    """For dam_sparse_attn_decode_quantized, or the grouped form and plans (shared_lists, max_kept = max_entries)."""
+    p = decode_params(q, cache.k, q, 0.0, shared_lists)
+    f = lib().dam_sparse_attn_decode_grouped_quantized_workspace if grouped else lib().dam_sparse_attn_decode_quantized_workspace
+    return torch.empty(max(f(ctypes.byref(p), max_kept), 256), dtype=torch.uint8, device=q.device)
+
+
+def dam_sparse_attn_decode_quantized(q, cache: QuantCache, kept_ptr, kept_idx, max_kept: int, out=None, lse=None,
+                                     scale: float = 0.0, ws=None, want_lse: bool = False, shared_lists: bool = False):
+    """dam_sparse_attn_decode over a cache of 8-bit codes."""
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = decode_quantized_workspace(q, cache, max_kept, False, shared_lists)
+    st = (_native or native()).decode_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q, kept_ptr, kept_idx,
+                                                None, max_kept, out, lse, scale, shared_lists, ws)
+    if st:
+        _check("dam_sparse_attn_decode_quantized", st)
+    return (out, lse) if (want_lse or lse is not None) else out
+
+
+def dam_sparse_attn_decode_grouped_quantized(q, cache: QuantCache, kept_ptr, kept_idx, kept_member, max_kept: int, out=None,
+                                             lse=None, scale: float = 0.0, ws=None, want_lse: bool = False,
+                                             shared_lists: bool = False):
+    """dam_sparse_attn_decode_grouped over a cache of 8-bit codes."""
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = decode_quantized_workspace(q, cache, max_kept, True, shared_lists)
+    assert kept_member is not None, "dam_sparse_attn_decode_grouped_quantized: member bits are wanted beside the lists"
+    st = (_native or native()).decode_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q, kept_ptr, kept_idx,
+                                                kept_member, max_kept, out, lse, scale, shared_lists, ws)
+    if st:
+        _check("dam_sparse_attn_decode_grouped_quantized", st)
+    return (out, lse) if (want_lse or lse is not None) else out
+
+
+def dam_sparse_attn_decode_patterns_quantized(q, cache: QuantCache, plan: "Mask", pos: int, max_entries: int, out=None,
+                                              lse=None, scale: float = 0.0, ws=None, want_lse: bool = False):
+    """dam_sparse_attn_decode_patterns over a cache of 8-bit codes."""
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = decode_quantized_workspace(q, cache, max_entries, True, True)
+    st = (_native or native()).decode_patterns_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q,
+                                                         plan.kept_ptr, plan.kept_idx, plan.kept_member, plan.plan_table, pos,
+                                                         max_entries, out, lse, scale, ws)
+    if st:
+        _check("dam_sparse_attn_decode_patterns_quantized", st)
+    return (out, lse) if (want_lse or lse is not None) else out
 
 
 # ---------------------------------------------------------------------------------------------

@@ -1,0 +1,302 @@
+// dam_kv_quantize, dam_kv_dequantize: rows of K and V into a cache of 8-bit codes as they are made, and back.
+//
+// Mathematics: dam_quant.h. For a block of rows with the largest finite magnitude a among the new ones,
+//   s = max(smallest s' with a <= c_max 2^(s' - 127), the block's scale if it holds rows in front of the new ones),
+//   code = round(x 2^(127 - s)); the rows in front become round(code 2^(s_old - s)) where s has grown.
+// Both are bound by HBM: 2 d (sizeof(T) + 1) bytes a row against a handful of operations per element.
+//
+// One workgroup writes one block of rows of K or V of one (sequence, KV head): the new rows are read once into registers
+// (a row by d / 8 adjacent lanes), the largest magnitude goes through one barrier, and the codes are written from the
+// registers. No two workgroups share a block, so nothing is atomic and the result does not depend on any order.
+#include <hip/hip_bf16.h>
+
+#include <algorithm>
+
+#include "dam_internal.h"
+#include "dam_quant.h"
+
+namespace {
+using namespace dam;
+
+struct QuantArgs {
+  int B, Hkv, cap, n_rows, pos;
+  int n_blocks;         // blocks of the cache that n_rows rows can touch
+  int64_t n_units;      // workgroups' items: (sequence, KV head, K or V, block)
+  int64_t x_sb[2], x_sh[2], x_ss[2];  // element strides of k and v
+  int64_t c_sb, c_sh, c_ss, s_sb, s_sh;
+};
+
+// Where the rows of sequence b go. (The arrays are device data that the host cannot check: a start outside the cache has
+// no rows, and none are taken beyond the cache's end or the caller's rows.)
+struct Span {
+  int start, count;
+  __device__ Span(const QuantArgs &a, int b, const int *start_at, const int *count_at) {
+    start = start_at ? start_at[b] : a.pos;
+    count = count_at ? min(max(count_at[b], 0), a.n_rows) : a.n_rows;
+    if (start < 0 || start >= a.cap) start = 0, count = 0;
+    count = min(count, a.cap - start);
+  }
+};
+
+// Eight elements of a row as fp32.
+__device__ __forceinline__ void load8(const float *p, float *v) {
+  const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __hip_bfloat16 *p, float *v) {
+  const uint4 a = *reinterpret_cast<const uint4 *>(p);
+  const unsigned u[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store8(float *p, const float *v) {
+  reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(__hip_bfloat16 *p, const float *v) {  // (values of the cache are bf16 numbers)
+  unsigned u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xFFFF0000u);
+  *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+template <typename T, int FORMAT, int D, int BLK>
+__global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a, const T *__restrict__ k, const T *__restrict__ v,
+                                                     const int *__restrict__ start_at, const int *__restrict__ count_at,
+                                                     uint8_t *kcache, uint8_t *vcache, uint8_t *kscale, uint8_t *vscale) {
+  using C = Code<FORMAT>;
+  constexpr int LPR = D / 8;                                // lanes per row
+  constexpr int THREADS = BLK * LPR < 256 ? BLK * LPR : 256;
+  constexpr int ROWS = THREADS / LPR, PASSES = BLK / ROWS;  // rows at a time
+  __shared__ unsigned s_top[THREADS / 64 + 1];
+  const int lane8 = threadIdx.x % LPR * 8, row0 = threadIdx.x / LPR;
+  for (int64_t unit = blockIdx.x; unit < a.n_units; unit += gridDim.x) {
+    const int nth = (int)(unit % a.n_blocks);
+    const int64_t rest = unit / a.n_blocks;
+    const int h = (int)(rest % a.Hkv), is_v = (int)(rest / a.Hkv % 2), b = (int)(rest / a.Hkv / 2);
+    const Span span(a, b, start_at, count_at);
+    const int block = span.start / BLK + nth, first = block * BLK;  // first row of the block
+    if (first >= span.start + span.count) continue;                 // (the whole workgroup)
+    const T *x = (is_v ? v : k) + b * a.x_sb[is_v] + h * a.x_sh[is_v] + lane8;
+    uint8_t *codes = (is_v ? vcache : kcache) + b * a.c_sb + h * a.c_sh + first * a.c_ss + lane8;
+    uint8_t *scale = (is_v ? vscale : kscale) + b * a.s_sb + h * a.s_sh + block;
+
+    float val[PASSES][8];
+    unsigned row_top[PASSES], top = 0;  // bits of the largest magnitude: of the row, of this lane's finite rows
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int rel = first + p * ROWS + row0 - span.start;  // row among the new ones
+#pragma unroll
+      for (int e = 0; e < 8; ++e) val[p][e] = 0.0f;
+      if (rel >= 0 && rel < span.count) load8(x + rel * a.x_ss[is_v], val[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      unsigned t = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(val[p][e]) & 0x7FFFFFFFu);
+      for (int off = 1; off < LPR; off <<= 1) t = max(t, (unsigned)__shfl_xor((int)t, off));
+      row_top[p] = t;
+      if (t < 0x7F800000u) top = max(top, t);
+    }
+    for (int off = LPR; off < 64; off <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, off));
+    if (threadIdx.x % 64 == 0) s_top[threadIdx.x / 64] = top;
+    if (threadIdx.x == 0) s_top[THREADS / 64] = first < span.start ? *scale : 0u;  // (no rows in front: a new block)
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) top = max(top, s_top[w]);
+    const unsigned old = s_top[THREADS / 64], s = max(C::need(top), old);
+    const float down = s ? __uint_as_float((254u - s) << 23) : 0.0f;  // 2^(127 - s)
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int rel = first + p * ROWS + row0 - span.start;
+      uint2 *at = reinterpret_cast<uint2 *>(codes + (int64_t)(p * ROWS + row0) * a.c_ss);
+      if (rel >= 0 && rel < span.count) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) val[p][e] *= down;
+        const unsigned nan = C::kNan * 0x01010101u;
+        const bool bad = row_top[p] >= 0x7F800000u;
+        *at = bad ? make_uint2(nan, nan) : pack8<FORMAT>(val[p], s);
+      } else if (rel < 0 && s > old) {  // a row in front, to the larger scale
+        const uint2 was = *at;
+        if (!C::is_nan(was.x)) {
+          float c[8];
+          C::unpack4(was.x, c);
+          C::unpack4(was.y, c + 4);
+          const float shift = old ? ldexpf(1.0f, (int)old - (int)s) : 0.0f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) c[e] *= shift;
+          *at = pack8<FORMAT>(c, s);
+        }
+      }
+    }
+    if (threadIdx.x == 0) *scale = (uint8_t)s;
+    __syncthreads();  // s_top is taken again
+  }
+}
+
+template <typename T, int FORMAT, int D>
+__global__ __launch_bounds__(256) void k_kv_dequantize(QuantArgs a, int shift, const uint8_t *__restrict__ kcache,
+                                                       const uint8_t *__restrict__ vcache, const uint8_t *__restrict__ kscale,
+                                                       const uint8_t *__restrict__ vscale, const int *__restrict__ start_at,
+                                                       const int *__restrict__ count_at, T *__restrict__ k, T *__restrict__ v) {
+  using C = Code<FORMAT>;
+  constexpr int LPR = D / 8, ROWS = 256 / LPR, PASSES = 4;
+  const int lane8 = threadIdx.x % LPR * 8, row0 = threadIdx.x / LPR;
+  for (int64_t unit = blockIdx.x; unit < a.n_units; unit += gridDim.x) {
+    const int nth = (int)(unit % a.n_blocks);
+    const int64_t rest = unit / a.n_blocks;
+    const int h = (int)(rest % a.Hkv), is_v = (int)(rest / a.Hkv % 2), b = (int)(rest / a.Hkv / 2);
+    const Span span(a, b, start_at, count_at);
+    const uint8_t *codes = (is_v ? vcache : kcache) + b * a.c_sb + h * a.c_sh + lane8;
+    const uint8_t *scale = (is_v ? vscale : kscale) + b * a.s_sb + h * a.s_sh;
+    T *x = (is_v ? v : k) + b * a.x_sb[is_v] + h * a.x_sh[is_v] + lane8;
+    uint2 c[PASSES];
+    unsigned s[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int rel = (nth * PASSES + p) * ROWS + row0;
+      if (rel < span.count) {
+        c[p] = *reinterpret_cast<const uint2 *>(codes + (int64_t)(span.start + rel) * a.c_ss);
+        s[p] = scale[(span.start + rel) >> shift];
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int rel = (nth * PASSES + p) * ROWS + row0;
+      if (rel >= span.count) continue;
+      float val[8];
+      C::unpack4(c[p].x, val);
+      C::unpack4(c[p].y, val + 4);
+      const float f = C::is_nan(c[p].x) ? NAN : scale_value(s[p]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) val[e] *= f;
+      store8(x + rel * a.x_ss[is_v], val);
+    }
+  }
+}
+
+constexpr int kMostRows = INT32_MAX - 1024;  // row numbers of whole blocks stay within 32 bits
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// `write`: the caches and scales are written, else k and v are.
+int validate(const dam_quant_params *p, const dam_quant_cache *c, const void *k, const void *v, bool write) {
+  if (!p || !c || (p->n_rows != 0 && (!k || !v)) || !c->kcache || !c->vcache || !c->kscale || !c->vscale) return DAM_ERR_INVALID_ARG;
+  if (p->batch < 1 || p->hkv < 1 || p->kv_capacity < 1 || p->n_rows < 0 || p->pos < 0 || p->pos > p->kv_capacity)
+    return DAM_ERR_INVALID_ARG;
+  if (p->kv_capacity > kMostRows || p->n_rows > kMostRows) return DAM_ERR_UNSUPPORTED;
+  if (p->dtype != DAM_F32 && p->dtype != DAM_BF16) return DAM_ERR_UNSUPPORTED;
+  if (p->head_dim != 64 && p->head_dim != 128) return DAM_ERR_UNSUPPORTED;
+  if (!quant_format_ok(c->format, c->block)) return DAM_ERR_UNSUPPORTED;
+  const int per16 = p->dtype == DAM_BF16 ? 8 : 4;
+  for (int i = 0; i < 3; ++i)
+    if (p->k_stride[i] < 0 || p->k_stride[i] % per16 || p->v_stride[i] < 0 || p->v_stride[i] % per16 || p->kv_stride[i] < 0 ||
+        p->kv_stride[i] % 16)
+      return DAM_ERR_INVALID_ARG;
+  if (c->scale_stride[0] < 0 || c->scale_stride[1] < 0) return DAM_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(c->kcache) || !aligned16(c->vcache)) return DAM_ERR_INVALID_ARG;
+  // what is written must not lie on top of itself
+  const int n[3] = {p->batch, p->hkv, write ? p->kv_capacity : p->n_rows};
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] < 2) continue;
+    const int64_t least = i == 2 ? p->head_dim : 1;
+    if (write ? p->kv_stride[i] < least || (i < 2 && c->scale_stride[i] < 1) : p->k_stride[i] < least || p->v_stride[i] < least)
+      return DAM_ERR_INVALID_ARG;
+  }
+  return DAM_OK;
+}
+
+QuantArgs make_args(const dam_quant_params *p, const dam_quant_cache *c, int64_t n_blocks) {
+  QuantArgs a;
+  a.B = p->batch; a.Hkv = p->hkv; a.cap = p->kv_capacity; a.n_rows = p->n_rows; a.pos = p->pos;
+  a.n_blocks = (int)n_blocks;
+  a.n_units = n_blocks * p->hkv * 2 * p->batch;
+  a.x_sb[0] = p->k_stride[0]; a.x_sh[0] = p->k_stride[1]; a.x_ss[0] = p->k_stride[2];
+  a.x_sb[1] = p->v_stride[0]; a.x_sh[1] = p->v_stride[1]; a.x_ss[1] = p->v_stride[2];
+  a.c_sb = p->kv_stride[0]; a.c_sh = p->kv_stride[1]; a.c_ss = p->kv_stride[2];
+  a.s_sb = c->scale_stride[0]; a.s_sh = c->scale_stride[1];
+  return a;
+}
+
+// (a launch holds fewer than 2^32 threads)
+int grid_of(const QuantArgs &a) { return (int)std::min<int64_t>(a.n_units, 1 << 22); }
+
+template <typename T, int FORMAT, int D, int BLK>
+void quantize(const QuantArgs &a, const dam_quant_cache *c, const void *k, const void *v, const int32_t *start,
+              const int32_t *count, hipStream_t st) {
+  constexpr int THREADS = BLK * (D / 8) < 256 ? BLK * (D / 8) : 256;
+  k_kv_quantize<T, FORMAT, D, BLK><<<grid_of(a), THREADS, 0, st>>>(
+      a, static_cast<const T *>(k), static_cast<const T *>(v), start, count, static_cast<uint8_t *>(c->kcache),
+      static_cast<uint8_t *>(c->vcache), c->kscale, c->vscale);
+}
+
+template <typename T, int FORMAT, int D>
+void quantize_by_block(const QuantArgs &a, const dam_quant_cache *c, const void *k, const void *v, const int32_t *start,
+                       const int32_t *count, hipStream_t st) {
+  if (c->block == 16) quantize<T, FORMAT, D, 16>(a, c, k, v, start, count, st);
+  else if (c->block == 32) quantize<T, FORMAT, D, 32>(a, c, k, v, start, count, st);
+  else if (c->block == 64) quantize<T, FORMAT, D, 64>(a, c, k, v, start, count, st);
+  else quantize<T, FORMAT, D, 128>(a, c, k, v, start, count, st);
+}
+
+template <typename T, int FORMAT, int D>
+void dequantize(const QuantArgs &a, const dam_quant_cache *c, const int32_t *start, const int32_t *count, void *k, void *v,
+                hipStream_t st) {
+  const int shift = c->block == 16 ? 4 : c->block == 32 ? 5 : c->block == 64 ? 6 : 7;
+  k_kv_dequantize<T, FORMAT, D><<<grid_of(a), 256, 0, st>>>(
+      a, shift, static_cast<const uint8_t *>(c->kcache), static_cast<const uint8_t *>(c->vcache), c->kscale, c->vscale, start,
+      count, static_cast<T *>(k), static_cast<T *>(v));
+}
+
+}  // namespace
+
+extern "C" int dam_kv_quantize(const dam_quant_params *p, const dam_quant_cache *cache, const void *k, const void *v,
+                               const int32_t *start, const int32_t *count, void *stream_v) {
+  const int bad = validate(p, cache, k, v, true);
+  if (bad != DAM_OK) return bad;
+  if (!start && !count && p->n_rows > p->kv_capacity - p->pos) return DAM_ERR_INVALID_ARG;
+  if (p->n_rows == 0) return DAM_OK;
+  // blocks that n rows touch where they start in a block's last row, and no more than the cache has
+  const int64_t n_blocks = std::min<int64_t>(((int64_t)p->n_rows + cache->block - 2) / cache->block + 1,
+                                             ((int64_t)p->kv_capacity + cache->block - 1) / cache->block);
+  const QuantArgs a = make_args(p, cache, n_blocks);
+  hipStream_t st = static_cast<hipStream_t>(stream_v);
+  const bool e4m3 = cache->format == DAM_KV_E4M3, wide = p->head_dim == 128;
+  if (p->dtype == DAM_BF16) {
+    if (e4m3 && wide) quantize_by_block<__hip_bfloat16, DAM_KV_E4M3, 128>(a, cache, k, v, start, count, st);
+    else if (e4m3) quantize_by_block<__hip_bfloat16, DAM_KV_E4M3, 64>(a, cache, k, v, start, count, st);
+    else if (wide) quantize_by_block<__hip_bfloat16, DAM_KV_INT8, 128>(a, cache, k, v, start, count, st);
+    else quantize_by_block<__hip_bfloat16, DAM_KV_INT8, 64>(a, cache, k, v, start, count, st);
+  } else {
+    if (e4m3 && wide) quantize_by_block<float, DAM_KV_E4M3, 128>(a, cache, k, v, start, count, st);
+    else if (e4m3) quantize_by_block<float, DAM_KV_E4M3, 64>(a, cache, k, v, start, count, st);
+    else if (wide) quantize_by_block<float, DAM_KV_INT8, 128>(a, cache, k, v, start, count, st);
+    else quantize_by_block<float, DAM_KV_INT8, 64>(a, cache, k, v, start, count, st);
+  }
+  return launch_status();
+}
+
+extern "C" int dam_kv_dequantize(const dam_quant_params *p, const dam_quant_cache *cache, const int32_t *start,
+                                 const int32_t *count, void *k, void *v, void *stream_v) {
+  const int bad = validate(p, cache, k, v, false);
+  if (bad != DAM_OK) return bad;
+  if (!start && !count && p->n_rows > p->kv_capacity - p->pos) return DAM_ERR_INVALID_ARG;
+  if (p->n_rows == 0) return DAM_OK;
+  const int rows = 4 * 256 / (p->head_dim / 8);  // of a workgroup
+  const QuantArgs a = make_args(p, cache, ((int64_t)p->n_rows + rows - 1) / rows);
+  hipStream_t st = static_cast<hipStream_t>(stream_v);
+  const bool e4m3 = cache->format == DAM_KV_E4M3, wide = p->head_dim == 128;
+  if (p->dtype == DAM_BF16) {
+    if (e4m3 && wide) dequantize<__hip_bfloat16, DAM_KV_E4M3, 128>(a, cache, start, count, k, v, st);
+    else if (e4m3) dequantize<__hip_bfloat16, DAM_KV_E4M3, 64>(a, cache, start, count, k, v, st);
+    else if (wide) dequantize<__hip_bfloat16, DAM_KV_INT8, 128>(a, cache, start, count, k, v, st);
+    else dequantize<__hip_bfloat16, DAM_KV_INT8, 64>(a, cache, start, count, k, v, st);
+  } else {
+    if (e4m3 && wide) dequantize<float, DAM_KV_E4M3, 128>(a, cache, start, count, k, v, st);
+    else if (e4m3) dequantize<float, DAM_KV_E4M3, 64>(a, cache, start, count, k, v, st);
+    else if (wide) dequantize<float, DAM_KV_INT8, 128>(a, cache, start, count, k, v, st);
+    else dequantize<float, DAM_KV_INT8, 64>(a, cache, start, count, k, v, st);
+  }
+  return launch_status();
+}

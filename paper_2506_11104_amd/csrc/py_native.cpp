@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kBadDtype = -1000;    // a query tensor that is neither fp32 nor bf16
 constexpr int kBadLayout = -1001;   // strides or shapes the wrappers rule out by assertion
+constexpr int kBadDevice = -1002;   // a tensor that is not on the current device
 
 void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
@@ -243,9 +244,162 @@ PyObject *decode_patterns(PyObject *const *a, Py_ssize_t n) {
                                                 d.ws.bytes(), stream());
 }
 
+// The tensors of a cache of 8-bit codes: K and V codes [batch][hkv][capacity][head_dim] with identical strides, scales
+// [batch][hkv][at least ceil(capacity / block)] with identical strides, rows per scale.
+struct QuantCache {
+  Arg kc, vc, ks, vs;
+  int64_t block = 0;
+  dam_quant_cache c{};
+  int bad = 0;
+  bool ok;
+  explicit QuantCache(PyObject *const *a) : kc(a[0]), vc(a[1]), ks(a[2]), vs(a[3]) {
+    ok = kc.ok && vc.ok && ks.ok && vs.ok && number(a[4], &block);
+    if (!ok) return;
+    const auto type = kc.t->scalar_type();
+    if (vc.t->scalar_type() != type || (type != at::kFloat8_e4m3fn && type != at::kChar) || ks.t->scalar_type() != at::kByte ||
+        vs.t->scalar_type() != at::kByte) {
+      bad = kBadDtype;
+    } else if (kc.dim() != 4 || ks.dim() != 3 || kc.t->sizes() != vc.t->sizes() || kc.t->strides() != vc.t->strides() ||
+               ks.t->sizes() != vs.t->sizes() || ks.t->strides() != vs.t->strides() || kc.stride(3) != 1 ||
+               (ks.size(2) > 1 && ks.stride(2) != 1) || ks.size(0) != kc.size(0) || ks.size(1) != kc.size(1) || block < 1 ||
+               ks.size(2) < (kc.size(2) + block - 1) / block) {
+      bad = kBadLayout;
+    }
+    c.kcache = kc.ptr(), c.vcache = vc.ptr(), c.kscale = (uint8_t *)ks.ptr(), c.vscale = (uint8_t *)vs.ptr();
+    c.format = type == at::kFloat8_e4m3fn ? DAM_KV_E4M3 : DAM_KV_INT8;
+    c.block = (int32_t)block;
+    if (!bad) c.scale_stride[0] = ks.stride(0), c.scale_stride[1] = ks.stride(1);
+  }
+};
+
+bool on_current_device(std::initializer_list<const Arg *> tensors) {
+  for (const Arg *x : tensors)
+    if (x->t && !x->t->is_cuda()) return false;
+  const auto current = c10::hip::current_device();  // (throws where there is no GPU)
+  for (const Arg *x : tensors)
+    if (x->t && x->t->get_device() != current) return false;
+  return true;
+}
+
+// A contiguous tensor of that type and of n elements at least (n < 0: any number), or None.
+bool flat(const Arg &x, at::ScalarType type, int64_t n = -1) {
+  return !x.t || (x.t->scalar_type() == type && x.t->is_contiguous() && x.t->numel() >= n);
+}
+
+// (kcache, vcache, kscale, vscale, block, k, v, pos, start, count, write)
+PyObject *kv_rows(PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 11)) return nullptr;
+  const QuantCache cache(a);
+  if (!cache.ok) return nullptr;
+  const Arg k(a[5]), v(a[6]), start(a[8], true), count(a[9], true);
+  int64_t pos;
+  const int write = PyObject_IsTrue(a[10]);
+  if (!k.ok || !v.ok || !start.ok || !count.ok || write < 0 || !number(a[7], &pos)) return nullptr;
+  if (cache.bad) return status(cache.bad);
+  dam_quant_params p{};
+  p.dtype = dtype_code(k);
+  if (p.dtype < 0 || v.t->scalar_type() != k.t->scalar_type()) return status(kBadDtype);
+  if (k.dim() != 4 || k.t->sizes() != v.t->sizes() || k.stride(3) != 1 || v.stride(3) != 1 || k.size(0) != cache.kc.size(0) ||
+      k.size(1) != cache.kc.size(1) || k.size(3) != cache.kc.size(3) || !flat(start, at::kInt, k.size(0)) ||
+      !flat(count, at::kInt, k.size(0)) || pos != (int32_t)pos)
+    return status(kBadLayout);
+  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &k, &v, &start, &count})) return status(kBadDevice);
+  p.batch = (int32_t)k.size(0);
+  p.hkv = (int32_t)k.size(1);
+  p.kv_capacity = (int32_t)cache.kc.size(2);
+  p.head_dim = (int32_t)k.size(3);
+  p.n_rows = (int32_t)k.size(2);
+  p.pos = (int32_t)pos;
+  for (int i = 0; i < 3; ++i) p.k_stride[i] = k.stride(i), p.v_stride[i] = v.stride(i), p.kv_stride[i] = cache.kc.stride(i);
+  const int32_t *s = (const int32_t *)start.ptr(), *c = (const int32_t *)count.ptr();
+  return write ? call(dam_kv_quantize, &p, &cache.c, (const void *)k.ptr(), (const void *)v.ptr(), s, c, stream())
+               : call(dam_kv_dequantize, &p, &cache.c, s, c, k.ptr(), v.ptr(), stream());
+}
+
+// The tensors and numbers of the decodes over such a cache.
+struct QuantDecode {
+  Arg q, out, lse, ws;
+  dam_decode_params p{};
+  int bad = 0;
+  bool ok;
+  QuantDecode(const QuantCache &cache, PyObject *q_, PyObject *out_, PyObject *lse_, PyObject *ws_, PyObject *scale_, bool shared)
+      : q(q_), out(out_), lse(lse_, true), ws(ws_, true) {
+    float scale;
+    ok = q.ok && out.ok && lse.ok && ws.ok && number(scale_, &scale);
+    if (!ok) return;
+    p.dtype = dtype_code(q);
+    if (cache.bad || p.dtype < 0 || out.t->scalar_type() != q.t->scalar_type()) {
+      bad = cache.bad ? cache.bad : kBadDtype;
+      return;
+    }
+    if (q.dim() != 3 || out.t->sizes() != q.t->sizes() || q.stride(2) != 1 || out.stride(2) != 1 ||
+        q.size(0) != cache.kc.size(0) || q.size(2) != cache.kc.size(3) || !flat(lse, at::kFloat, q.size(0) * q.size(1)) ||
+        !flat(ws, at::kByte)) {
+      bad = kBadLayout;
+      return;
+    }
+    p.batch = (int32_t)q.size(0);
+    p.hq = (int32_t)q.size(1);
+    p.hkv = (int32_t)cache.kc.size(1);
+    p.kv_capacity = (int32_t)cache.kc.size(2);
+    p.head_dim = (int32_t)q.size(2);
+    p.scale = scale;
+    for (int i = 0; i < 2; ++i) p.q_stride[i] = q.stride(i), p.o_stride[i] = out.stride(i);
+    for (int i = 0; i < 3; ++i) p.kv_stride[i] = cache.kc.stride(i);
+    p.shared_lists = shared ? 1 : 0;
+  }
+};
+
+// (kcache, vcache, kscale, vscale, block, q, kept_ptr, kept_idx, kept_member, max_kept, out, lse, scale, shared, ws)
+// kept_member None: a list per query head; else merged lists per KV head.
+PyObject *decode_quantized(PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 15)) return nullptr;
+  const QuantCache cache(a);
+  if (!cache.ok) return nullptr;
+  const Arg ptr(a[6]), idx(a[7], true), mem(a[8], true);
+  int64_t max_kept;
+  const int shared = PyObject_IsTrue(a[13]);
+  if (!ptr.ok || !idx.ok || !mem.ok || shared < 0 || !number(a[9], &max_kept)) return nullptr;
+  const QuantDecode d(cache, a[5], a[10], a[11], a[14], a[12], shared != 0);
+  if (!d.ok) return nullptr;
+  if (d.bad) return status(d.bad);
+  const int64_t lists = (mem.t ? d.p.hkv : d.p.hq) * (int64_t)(shared ? 1 : d.p.batch);
+  if (!flat(ptr, at::kInt, lists + 1) || !flat(idx, at::kInt) || !flat(mem, at::kByte)) return status(kBadLayout);
+  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &d.q, &d.out, &d.lse, &d.ws, &ptr, &idx, &mem}))
+    return status(kBadDevice);
+  const int32_t *kp = (const int32_t *)ptr.ptr(), *ki = (const int32_t *)idx.ptr();
+  if (mem.t)
+    return call(dam_sparse_attn_decode_grouped_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, kp, ki, (const uint8_t *)mem.ptr(),
+                max_kept, d.out.ptr(), (float *)d.lse.ptr(), d.ws.ptr(), d.ws.bytes(), stream());
+  return call(dam_sparse_attn_decode_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, kp, ki, max_kept, d.out.ptr(),
+              (float *)d.lse.ptr(), d.ws.ptr(), d.ws.bytes(), stream());
+}
+
+// (kcache, vcache, kscale, vscale, block, q, plan_ptr, plan_val, plan_member, plan_table, pos, max_entries, out, lse, scale, ws)
+PyObject *decode_patterns_quantized(PyObject *const *a, Py_ssize_t n) {
+  if (!arity(n, 16)) return nullptr;
+  const QuantCache cache(a);
+  if (!cache.ok) return nullptr;
+  const Arg ptr(a[6]), val(a[7], true), mem(a[8], true), tab(a[9]);
+  int64_t pos, most;
+  if (!ptr.ok || !val.ok || !mem.ok || !tab.ok || !number(a[10], &pos) || !number(a[11], &most)) return nullptr;
+  const QuantDecode d(cache, a[5], a[12], a[13], a[15], a[14], true);
+  if (!d.ok) return nullptr;
+  if (d.bad) return status(d.bad);
+  if (!flat(ptr, at::kInt, d.p.hkv + 1) || !flat(val, at::kInt) || !flat(mem, at::kByte) || !flat(tab, at::kByte) ||
+      tab.dim() != 2 || tab.size(0) < d.p.hkv || pos != (int32_t)pos)
+    return status(kBadLayout);
+  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &d.q, &d.out, &d.lse, &d.ws, &ptr, &val, &mem, &tab}))
+    return status(kBadDevice);
+  return call(dam_sparse_attn_decode_patterns_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, (const int32_t *)ptr.ptr(),
+              (const int32_t *)val.ptr(), (const uint8_t *)mem.ptr(), (const uint8_t *)tab.ptr(), (int32_t)tab.size(1), (int32_t)pos,
+              most, d.out.ptr(), (float *)d.lse.ptr(), d.ws.ptr(), d.ws.bytes(), stream());
+}
+
 #define DAM_FN(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DAM_FN(mask_build), DAM_FN(mask_build_from_qk), DAM_FN(capture_accumulate), DAM_FN(prefill), DAM_FN(decode),
-                         DAM_FN(decode_patterns), {nullptr, nullptr, 0, nullptr}};
+                         DAM_FN(decode_patterns), DAM_FN(kv_rows), DAM_FN(decode_quantized), DAM_FN(decode_patterns_quantized),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dam_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
