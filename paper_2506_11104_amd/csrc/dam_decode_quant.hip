@@ -321,10 +321,22 @@ int validate_grouped(const dam_decode_params *p, const void *q, const dam_quant_
   return DAM_OK;
 }
 
+// Workgroups of a list, and the waves of each where the call takes the matrix-core kernel (`mfma`): eight waves per CU in
+// workgroups of four, each wave with at least one block of 32 entries. Up to four waves are one workgroup.
+GroupSplit splits_of(const dam_decode_params *p, int64_t max_kept, bool grouped, bool *mfma) {
+  const int64_t lists = (int64_t)p->batch * (grouped ? p->hkv : p->hq);
+  *mfma = grouped && decode_quant_mfma_fits(p);
+  if (!*mfma) return {4, pick_splits(lists, max_kept)};
+  const int64_t s = std::min<int64_t>((2048 + lists - 1) / lists, std::max<int64_t>(1, max_kept / 32));
+  if (s <= 4) return {(int)s, 1};
+  const int64_t groups = std::min<int64_t>(512 / lists, max_kept / 128);
+  return {4, (int)std::min<int64_t>(std::max<int64_t>(groups, 1), 32)};
+}
+
 // What a call writes to its workspace; lists of query heads, or of KV heads.
 Partials partials(void *ws, const dam_decode_params *p, int64_t max_kept, bool grouped) {
-  const int64_t lists = (int64_t)p->batch * (grouped ? p->hkv : p->hq);
-  return Partials(ws, p, pick_splits(lists, max_kept), lists);
+  bool mfma;
+  return Partials(ws, p, splits_of(p, max_kept, grouped, &mfma).groups, (int64_t)p->batch * (grouped ? p->hkv : p->hq));
 }
 
 struct Plan {
@@ -375,16 +387,21 @@ int run(const Call &x, int64_t max_kept, bool grouped, void *ws) {
   a.shared_lists = p->shared_lists != 0;
   a.rows_of_kv = grouped ? 1 : p->hq / p->hkv;
   a.G = grouped ? p->hq / p->hkv : 1;
-  a.splits = pick_splits((int64_t)p->batch * p->hkv * a.rows_of_kv, max_kept);
+  bool mfma;
+  const GroupSplit split = splits_of(p, max_kept, grouped, &mfma);
+  a.splits = split.groups;
   a.block_shift = x.c->block == 16 ? 4 : x.c->block == 32 ? 5 : x.c->block == 64 ? 6 : 7;
   a.pos = x.plan.pos; a.n_flags = x.plan.n_flags;
-  a.flag = a.splits > 1 ? fresh_flag() : 0;
   a.scale = p->scale > 0.0f ? p->scale : 1.0f / sqrtf((float)p->head_dim);
   a.q_sb = p->q_stride[0]; a.q_sh = p->q_stride[1];
   a.kv_sb = p->kv_stride[0]; a.kv_sh = p->kv_stride[1]; a.kv_ss = p->kv_stride[2];
   a.s_sb = x.c->scale_stride[0]; a.s_sh = x.c->scale_stride[1];
   a.o_sb = p->o_stride[0]; a.o_sh = p->o_stride[1];
   const Partials part = partials(ws, p, max_kept, grouped);
+  if (mfma)
+    return launch_decode_quant_mfma(p, split, a.scale, x.q, x.c, a.block_shift, x.kept_ptr, x.kept_idx, x.kept_member, part.o,
+                                    part.ml, part.flags, x.out, x.lse, x.st, x.plan.table, x.plan.n_flags, x.plan.pos);
+  a.flag = a.splits > 1 ? fresh_flag() : 0;
   const bool e4m3 = x.c->format == DAM_KV_E4M3, wide = p->head_dim == 128;
   if (p->dtype == DAM_BF16) {
     if (e4m3 && wide) launch_form<__hip_bfloat16, DAM_KV_E4M3, 128>(x, a, part);
