@@ -33,7 +33,8 @@ constexpr int kEntries = 4 * kSlot;         // then four slots of 32 list entrie
 constexpr int kScales = kEntries + 4 * 256; // four slots of 32 words with a K scale, 32 with a V scale
 constexpr int kFix = kScales + 4 * 256;     // PLAN: four slots of plan-table words
 constexpr int kFloat = kFix + 4 * 256;      // the block's 32 V scales (and K scales) as fp32
-constexpr int kLds = kFloat + 256;
+constexpr int kMember = kFloat + 256;       // member bytes of the next block's keys, by key
+constexpr int kLds = kMember + 64;
 constexpr int kPart = 8 * 32 * 16;          // a wave's results: O of at most 8 heads at 0, what columns 16.. add to it here,
 constexpr int kMl = 2 * kPart;              // (reference, sum) here
 
@@ -53,9 +54,19 @@ __device__ __forceinline__ void lds_copy4_at(unsigned lds_at, uint64_t addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_at), "v"(addr) : "memory", "m0");
 }
 
-// Bits 0 and 2 exchanged: the order of a block's keys among the LDS rows. The two half-waves read V keys that differ in bit
-// 2, whose rows then lie in different halves of the banks.
-__device__ __forceinline__ int swap02(int r) { return (r & ~5) | ((r & 1) << 2) | ((r >> 2) & 1); }
+// Where the 16-byte chunk c of row r of a block lies in its LDS row: at position c ^ spread(r). Sixteen rows read at one
+// chunk, as K's operand does, and eight rows {0..3, 8..11} or {4..7, 12..15} read at two chunks 2 i and 2 i + 1, as V's does,
+// then touch every bank once.
+__device__ __forceinline__ int spread(int r) { return ((r >> 3) & 1) << 2 | ((r >> 1) & 1) << 1 | ((r >> 2) & 1); }
+
+// All ones where bit POS of a word is clear.
+__device__ __forceinline__ unsigned unset(unsigned w, int pos) { return ~(unsigned)__builtin_amdgcn_sbfe((int)w, pos, 1); }
+
+__device__ __forceinline__ u32x2 lds_read_tr8(const unsigned char *lds, int byte) {
+  typedef __attribute__((ext_vector_type(2))) int i32x2;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                       (__attribute__((address_space(3))) i32x2 *)(const_cast<unsigned char *>(lds + byte))));
+}
 
 // Codes 2 i and 2 i + 1 of a word, as two bf16 numbers, times a scale (e4m3 only).
 template <int FORMAT>
@@ -142,30 +153,55 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + kFix + (i & 3) * 256), addr);
     };
     // Scales and rows of local block i: one copy of the words that hold the 32 keys' scale bytes, four of K rows and four of
-    // V rows into slot i & 1. Copy `it` fills LDS rows 8 it .. 8 it + 7; row r holds key swap02(r), the 16-byte chunk c of a
-    // K row at position c ^ ((r >> 1) & 7), so that sixteen lanes with rows of their own read all banks.
+    // V rows into slot i & 1, LDS row r for key r of the block. Returns where in those words the scale bytes of key lane & 31
+    // lie (bits of K's, and of V's from bit 8 on).
     auto copy_rows = [&](int i) {
       const unsigned k_at = __builtin_amdgcn_readfirstlane(lds_base + (i & 1) * kSlot);
       const unsigned v_at = k_at + kVSlots;
-      unsigned koff[4], voff[4];
+      unsigned off[4];
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
         const int r = 8 * it + sub;
         // (row index and row stride are below 2^24: the 24-bit multiply runs at full rate, the 32-bit one does not)
-        const unsigned row_at = __umul24((unsigned)row_of(entry(i, swap02(r))), a.row_bytes);
-        koff[it] = row_at + ((pos ^ ((r >> 1) & 7)) << 4);
-        voff[it] = row_at + (pos << 4);
+        off[it] = __umul24((unsigned)row_of(entry(i, r)), a.row_bytes) + ((pos ^ spread(r)) << 4);
       }
-      const unsigned s = (unsigned)row_of(entry(i, lane & 31)) >> a.block_shift;
-      lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + kScales + (i & 3) * 256), ((lane < 32 ? ks_at : vs_at) + s) & ~(uint64_t)3);
-      lds_copy16_once<0 * 1024>(k_at, kg, koff[0]);
-      lds_copy16_once<1 * 1024>(k_at, kg, koff[1]);
-      lds_copy16_once<2 * 1024>(k_at, kg, koff[2]);
-      lds_copy16_once<3 * 1024>(k_at, kg, koff[3]);
-      lds_copy16_once<0 * 1024>(v_at, vg, voff[0]);
-      lds_copy16_once<1 * 1024>(v_at, vg, voff[1]);
-      lds_copy16_once<2 * 1024>(v_at, vg, voff[2]);
-      lds_copy16_once<3 * 1024>(v_at, vg, voff[3]);
+      const unsigned s = (unsigned)row_of(entry(i, n)) >> a.block_shift;
+      lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + kScales + (i & 3) * 256), ((hf ? vs_at : ks_at) + s) & ~(uint64_t)3);
+      lds_copy16_once<0 * 1024>(k_at, kg, off[0]);
+      lds_copy16_once<1 * 1024>(k_at, kg, off[1]);
+      lds_copy16_once<2 * 1024>(k_at, kg, off[2]);
+      lds_copy16_once<3 * 1024>(k_at, kg, off[3]);
+      lds_copy16_once<0 * 1024>(v_at, vg, off[0]);
+      lds_copy16_once<1 * 1024>(v_at, vg, off[1]);
+      lds_copy16_once<2 * 1024>(v_at, vg, off[2]);
+      lds_copy16_once<3 * 1024>(v_at, vg, off[3]);
+      return (((unsigned)ks_at + s) & 3) * 8 | (((unsigned)vs_at + s) & 3) * 0x800;
+    };
+    // Which heads keep which key of local block i (its entries and table words have landed): a byte per key, dealt out so
+    // that bit 8 (e % 4) of word e / 4 says whether this lane's head keeps the key of accumulator e, 8 (e / 4) + 4 hf + e % 4.
+    struct Kept {
+      unsigned w[4];
+    };
+    const int member_shift = (int)((member_at + (unsigned)lo) & 3);  // (blocks start a multiple of 32 entries apart)
+    auto keeps = [&](int i) {
+      unsigned mem = lds[kEntries + (i & 3) * 256 + 128 + member_shift + n];
+      if (entry0(i) + n >= end) mem = 0u;
+      if (PLAN) {
+        const int v = entry(i, n);
+        const bool exists = v < 0 ? a.pos + 1 + v >= 0 : v <= a.pos;
+        const int t = table_index(v);
+        unsigned covered = 0;  // heads that reach this column's key through a matched diagonal
+        if (t >= 0) {
+          const unsigned word = *reinterpret_cast<const unsigned *>(lds + kFix + (i & 3) * 256 + 4 * n);
+          covered = (word >> (8 * (int)((table_at + (unsigned)t) & 3))) & 0xFFu;
+        }
+        mem = exists ? mem & ~covered : 0u;
+      }
+      lds[kMember + n] = (unsigned char)mem;  // (both half-waves hold the same)
+      Kept k;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) k.w[g] = *reinterpret_cast<const unsigned *>(lds + kMember + 8 * g + 4 * hf) >> head;
+      return k;
     };
 
     // Q fragments: B operand of S^T = K Q^T. Column n is query head `head` of the group (zero beyond the group); fragment c
@@ -191,12 +227,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       if (nb > 1) copy_fix(1);
     }
     if (nb > 2) copy_entries(2);
-    copy_rows(0);
-    if (nb > 1) copy_rows(1);
+    unsigned bits_now = copy_rows(0), bits_next = 0;
+    if (nb > 1) bits_next = copy_rows(1);
 
-    const int krow = swap02(n);                         // LDS row of this lane's key
     const float lost = n >= 16 ? 1.0f : 0.0f;           // this column's weights are what bf16 loses
     float *vsf = reinterpret_cast<float *>(lds + kFloat), *ksf = vsf + 32;
+    // LDS byte offsets of this lane's operand fragments in a slot; the others differ by an XOR (and a2 by 2048 bytes). K: row n,
+    // chunks 4 hf .. 4 hf + 3. V: a transposing read takes eight bytes of a row per lane (lanes 2 r and 2 r + 1 of sixteen the 16
+    // bytes of row r of eight) and leaves a lane the byte of its own column of all eight rows: lane n dim 32 db + n of the
+    // keys 16 a2 + 4 hf + {0..3, 8..11}, the order in which the lane holds weights.
+    const int kbase = n * 128 + (((4 * hf) ^ spread(n)) << 4);
+    const int vrow = 4 * hf + ((lane >> 1) & 3) + 8 * ((lane >> 3) & 1);
+    const int vbase = vrow * 128 + ((((lane >> 4) & 1) ^ spread(vrow)) << 4) + 8 * (lane & 1);
+    Kept kept_now, kept_next;
 
     for (int i = 0; i < nb; ++i) {
       // The copies were issued in the order ... rows i, entries i + 2 (PLAN: table words i + 1), scales and rows i + 1: what
@@ -205,69 +248,48 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       if (i + 1 < nb) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       const unsigned char *kslot = lds + (i & 1) * kSlot;
-      unsigned char *vslot = lds + kVSlots + (i & 1) * kSlot;
-      const unsigned char *entries = lds + kEntries + (i & 3) * 256;
+      const unsigned char *vslot = lds + kVSlots + (i & 1) * kSlot;
 
-      // scales of key n of the block
-      const int v_n = entry(i, n);
-      const unsigned s_n = (unsigned)row_of(v_n) >> a.block_shift;
+      // Everything the block needs from LDS is asked for at once, for its latency to be paid once.
       const unsigned *words = reinterpret_cast<const unsigned *>(lds + kScales + (i & 3) * 256);
-      float kscale = scale_value((words[n] >> (8 * (int)((ks_at + s_n) & 3))) & 0xFFu);
-      float vscale = scale_value((words[32 + n] >> (8 * (int)((vs_at + s_n) & 3))) & 0xFFu);
-      // NaN rows: the scale carries the NaN, which reaches the heads that keep the row through the logits or the weights; a
-      // V row's codes are cleared, since the product would carry them to all heads
-      const bool vbad = C::is_nan(vslot[krow * 128]);
-      const unsigned vbads = (unsigned)__ballot(vbad);
-      if (vbads) {
-        if (vbad) {
-          vscale = NAN;
-          for (int c = hf; c < 8; c += 2) *reinterpret_cast<u32x4 *>(vslot + krow * 128 + 16 * c) = u32x4{0u, 0u, 0u, 0u};
-        }
-      }
-      if (hf == 0) vsf[n] = vscale;
-
-      // which heads keep which key: lane k < 32 holds the member byte of key k of the block
-      const int e0 = entry0(i);
-      const int shift = (int)((member_at + (unsigned)e0) & 3);
-      unsigned mem = lane < 32 && e0 + lane < end ? entries[128 + shift + lane] : 0u;
-      if (PLAN) {
-        const bool exists = v_n < 0 ? a.pos + 1 + v_n >= 0 : v_n <= a.pos;
-        const int t = table_index(v_n);
-        unsigned covered = 0;  // heads that reach this column's key through a matched diagonal
-        if (t >= 0) {
-          const unsigned word = *reinterpret_cast<const unsigned *>(lds + kFix + (i & 3) * 256 + 4 * n);
-          covered = (word >> (8 * (int)((table_at + (unsigned)t) & 3))) & 0xFFu;
-        }
-        mem = exists ? mem & ~covered : 0u;
-      }
-      unsigned mine = 0;  // bit k: key k of the block is kept by this lane's head
+      const unsigned kword = words[n], vword = words[32 + n], vfirst = vslot[n * 128];
+      u32x4 kw[4];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        if (x < G) {  // wave-uniform
-          const unsigned kept_x = (unsigned)__ballot((mem >> x) & 1);
-          if (head == x) mine = kept_x;
-        }
+      for (int j = 0; j < 4; ++j) kw[j] = *reinterpret_cast<const u32x4 *>(kslot + (kbase ^ (j << 4)));
+      if (i == 0) kept_now = keeps(0);
+      u32x2 vw[2][4];
+#pragma unroll
+      for (int a2 = 0; a2 < 2; ++a2)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) vw[a2][db] = lds_read_tr8(vslot, (vbase ^ (db << 5)) + 2048 * a2);
+
+      // Scales of key n of the block. NaN rows: the scale carries the NaN, which reaches the heads that keep the row through
+      // the logits (K's codes do so themselves in e4m3) or the weights; a V row's codes are cleared, since the product would
+      // carry them to all heads.
+      float kscale = scale_value((kword >> (bits_now & 31)) & 0xFFu);
+      float vscale = scale_value((vword >> (bits_now >> 8)) & 0xFFu);
+      const bool vbad = C::is_nan(vfirst);
+      if (vbad) vscale = NAN;
+      const unsigned vbads = (unsigned)__ballot(vbad);
+      if (kScaleOnLogits && C::is_nan(kw[0][0])) kscale = NAN;
+      if (hf == 0) {
+        vsf[n] = vscale;
+        if (kScaleOnLogits) ksf[n] = kscale;
       }
-      const int masked = (int)~(mine >> (4 * hf));  // bit 8 (e / 4) + e % 4: accumulator e's key is not kept
 
       // S^T = K Q^T; accumulator e is key 8 (e / 4) + 4 hf + e % 4
       f32x16 s;
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const u32x4 w = *reinterpret_cast<const u32x4 *>(kslot + krow * 128 + (((4 * hf + j) ^ ((krow >> 1) & 7)) << 4));
-        if (kScaleOnLogits && j == 0) {
-          if (C::is_nan(w[0])) kscale = NAN;
-          if (hf == 0) ksf[n] = kscale;
-        }
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const u32x4 f = {to_bf16<FORMAT>(w[2 * z], 0, kscale), to_bf16<FORMAT>(w[2 * z], 1, kscale),
-                           to_bf16<FORMAT>(w[2 * z + 1], 0, kscale), to_bf16<FORMAT>(w[2 * z + 1], 1, kscale)};
+          const u32x4 f = {to_bf16<FORMAT>(kw[j][2 * z], 0, kscale), to_bf16<FORMAT>(kw[j][2 * z], 1, kscale),
+                           to_bf16<FORMAT>(kw[j][2 * z + 1], 0, kscale), to_bf16<FORMAT>(kw[j][2 * z + 1], 1, kscale)};
           s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), qf[2 * j + z], s, 0, 0, 0);
         }
-      }
+      if (i + 1 < nb) kept_next = keeps(i + 1);
       if (kScaleOnLogits) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
@@ -275,9 +297,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
           s[4 * g] *= f.x, s[4 * g + 1] *= f.y, s[4 * g + 2] *= f.z, s[4 * g + 3] *= f.w;
         }
       }
-      // (after the products, so that a NaN row does not get past it)
+      // masked keys to -inf (after the products, so that a NaN row does not get past it)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = (masked >> (8 * (e / 4) + e % 4)) & 1 ? -INFINITY : s[e];
+      for (int e = 0; e < 16; ++e) {
+        const unsigned off = unset(kept_now.w[e / 4], 8 * (e % 4));
+        s[e] = __uint_as_float((off & 0xFF800000u) | (~off & __float_as_uint(s[e])));
+      }
 
       // online softmax, one head per lane pair (lane, lane ^ 32); the reference the weights are taken against
       // only moves when the maximum has grown past it by more than 8 in log2 units
@@ -307,15 +332,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
       for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -off));
 #pragma unroll
-      for (int e = 0; e < 16; ++e) l_run += w[e];
+      for (int g = 0; g < 4; ++g) l_run += (w[4 * g] + w[4 * g + 1]) + (w[4 * g + 2] + w[4 * g + 3]);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float4 f = *reinterpret_cast<const float4 *>(vsf + 8 * g + 4 * hf);
         w[4 * g] *= f.x, w[4 * g + 1] *= f.y, w[4 * g + 2] *= f.z, w[4 * g + 3] *= f.w;
       }
-      if (vbads) {  // (wave-uniform) a weight of 0 times a NaN scale
+      if (vbads) {  // (wave-uniform) a weight of 0 times a NaN scale; the rows' codes
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = (masked >> (8 * (e / 4) + e % 4)) & 1 ? 0.0f : w[e];
+        for (int e = 0; e < 16; ++e) w[e] = __uint_as_float(~unset(kept_now.w[e / 4], 8 * (e % 4)) & __float_as_uint(w[e]));
+#pragma unroll
+        for (int a2 = 0; a2 < 2; ++a2)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            // bits k of the keys in bytes k of the word
+            const unsigned gone = (((vbads >> (16 * a2 + 8 * z + 4 * hf)) & 15u) * 0x204081u & 0x01010101u) * 0xFFu;
+#pragma unroll
+            for (int db = 0; db < 4; ++db) vw[a2][db][z] &= ~gone;
+          }
       }
       // the upper 16 bits of a weight, or, in the columns from 16 on, those of what remains
       unsigned p[8];
@@ -326,36 +360,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         p[e / 2] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
       }
 
-      // O^T += V^T P^T. This lane reads dims 4 n .. 4 n + 3 of eight keys (LDS row hf + 2 (k >> 1 & 1) + 4 (k & 1) + 8 (k >> 2) +
-      // 16 a2 for the lane's key k); product db takes dim 4 n + db of each, so accumulator e of oacc[db] is dim
-      // 4 (8 (e / 4) + 4 hf + e % 4) + db.
+      // O^T += V^T P^T: accumulator e of dim block db is dim 32 db + 8 (e / 4) + 4 hf + e % 4
 #pragma unroll
       for (int a2 = 0; a2 < 2; ++a2) {
         const u32x4 praw = {p[4 * a2], p[4 * a2 + 1], p[4 * a2 + 2], p[4 * a2 + 3]};
-        unsigned d[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          d[k] = *reinterpret_cast<const unsigned *>(vslot + hf * 128 + 4 * n + 256 * ((k >> 1) & 1) + 512 * (k & 1) + 1024 * (k >> 2) + 2048 * a2);
-        u32x4 vf[4];
-#pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-          // bytes 0 and 1 of both keys side by side, then bytes 2 and 3
-          const unsigned t0 = __builtin_amdgcn_perm(d[k + 1], d[k], 0x05010400u), t1 = __builtin_amdgcn_perm(d[k + 1], d[k], 0x07030602u);
-          vf[0][k / 2] = to_bf16<FORMAT>(t0, 0, 1.0f);
-          vf[1][k / 2] = to_bf16<FORMAT>(t0, 1, 1.0f);
-          vf[2][k / 2] = to_bf16<FORMAT>(t1, 0, 1.0f);
-          vf[3][k / 2] = to_bf16<FORMAT>(t1, 1, 1.0f);
+        for (int db = 0; db < 4; ++db) {
+          const u32x2 x = vw[a2][db];
+          const u32x4 f = {to_bf16<FORMAT>(x[0], 0, 1.0f), to_bf16<FORMAT>(x[0], 1, 1.0f), to_bf16<FORMAT>(x[1], 0, 1.0f),
+                           to_bf16<FORMAT>(x[1], 1, 1.0f)};
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, praw), oacc[db],
+                                                             0, 0, 0);
         }
-#pragma unroll
-        for (int db = 0; db < 4; ++db)
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[db]), __builtin_bit_cast(bf16x8, praw),
-                                                             oacc[db], 0, 0, 0);
       }
       // every LDS read of block i has returned (the products consumed them): its slots are free for block i + 2
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      kept_now = kept_next;
+      bits_now = bits_next;
       if (i + 3 < nb) copy_entries(i + 3);
       if (PLAN && i + 2 < nb) copy_fix(i + 2);
-      if (i + 2 < nb) copy_rows(i + 2);
+      if (i + 2 < nb) bits_next = copy_rows(i + 2);
     }
   }
 
@@ -366,8 +390,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   if (head < G) {
     float4 *mine_o = reinterpret_cast<float4 *>(lds + (n >= 16 ? kPart : 0)) + head;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      mine_o[(8 * (e / 4) + 4 * hf + e % 4) * G] = make_float4(oacc[0][e], oacc[1][e], oacc[2][e], oacc[3][e]);
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        mine_o[(8 * db + 2 * g + hf) * G] =
+            make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]);
     if (lane < 16) reinterpret_cast<float2 *>(lds + kMl)[n] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * c2, l_tot);
   }
   __syncthreads();
