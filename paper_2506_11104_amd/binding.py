@@ -664,52 +664,42 @@ def decode_quantized_workspace(q, cache: QuantCache, max_kept: int, grouped: boo
 def dam_sparse_attn_decode_quantized(q, cache: QuantCache, kept_ptr, kept_idx, max_kept: int, out=None, lse=None,
                                      scale: float = 0.0, ws=None, want_lse: bool = False, shared_lists: bool = False):
     """dam_sparse_attn_decode over a cache of 8-bit codes."""
-    if out is None:
-        out = torch.empty_like(q)
-    if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
     if ws is None:
         ws = decode_quantized_workspace(q, cache, max_kept, False, shared_lists)
-    st = (_native or native()).decode_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q, kept_ptr, kept_idx,
-                                                None, max_kept, out, lse, scale, shared_lists, ws)
-    if st:
-        _check("dam_sparse_attn_decode_quantized", st)
-    return (out, lse) if (want_lse or lse is not None) else out
+    r = (_native or native()).decode_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q, kept_ptr, kept_idx,
+                                      None, max_kept, out, lse if lse is not None else want_lse or None, scale,
+                                      shared_lists, ws)
+    if isinstance(r, int):
+        _check("dam_sparse_attn_decode_quantized", r)
+    return r
 
 
 def dam_sparse_attn_decode_grouped_quantized(q, cache: QuantCache, kept_ptr, kept_idx, kept_member, max_kept: int, out=None,
                                              lse=None, scale: float = 0.0, ws=None, want_lse: bool = False,
                                              shared_lists: bool = False):
     """dam_sparse_attn_decode_grouped over a cache of 8-bit codes."""
-    if out is None:
-        out = torch.empty_like(q)
-    if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
     if ws is None:
         ws = decode_quantized_workspace(q, cache, max_kept, True, shared_lists)
     assert kept_member is not None, "dam_sparse_attn_decode_grouped_quantized: member bits are wanted beside the lists"
-    st = (_native or native()).decode_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q, kept_ptr, kept_idx,
-                                                kept_member, max_kept, out, lse, scale, shared_lists, ws)
-    if st:
-        _check("dam_sparse_attn_decode_grouped_quantized", st)
-    return (out, lse) if (want_lse or lse is not None) else out
+    r = (_native or native()).decode_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q, kept_ptr, kept_idx,
+                                      kept_member, max_kept, out, lse if lse is not None else want_lse or None, scale,
+                                      shared_lists, ws)
+    if isinstance(r, int):
+        _check("dam_sparse_attn_decode_grouped_quantized", r)
+    return r
 
 
 def dam_sparse_attn_decode_patterns_quantized(q, cache: QuantCache, plan: "Mask", pos: int, max_entries: int, out=None,
                                               lse=None, scale: float = 0.0, ws=None, want_lse: bool = False):
     """dam_sparse_attn_decode_patterns over a cache of 8-bit codes."""
-    if out is None:
-        out = torch.empty_like(q)
-    if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
     if ws is None:
         ws = decode_quantized_workspace(q, cache, max_entries, True, True)
-    st = (_native or native()).decode_patterns_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q,
-                                                         plan.kept_ptr, plan.kept_idx, plan.kept_member, plan.plan_table, pos,
-                                                         max_entries, out, lse, scale, ws)
-    if st:
-        _check("dam_sparse_attn_decode_patterns_quantized", st)
-    return (out, lse) if (want_lse or lse is not None) else out
+    r = (_native or native()).decode_patterns_quantized(cache.k, cache.v, cache.kscale, cache.vscale, cache.block, q,
+                                               plan.kept_ptr, plan.kept_idx, plan.kept_member, plan.plan_table, pos,
+                                               max_entries, out, lse if lse is not None else want_lse or None, scale, ws)
+    if isinstance(r, int):
+        _check("dam_sparse_attn_decode_patterns_quantized", r)
+    return r
 
 
 # ---------------------------------------------------------------------------------------------

@@ -2,293 +2,839 @@
 // keys of its own, over the merged list of its KV head's query heads, or over a plan of the matched patterns.
 //
 // Paper (arXiv 2506.11104): Sec. 3 (scaled dot-product attention) with the mask of Sec. 4.3 applied as -inf before the
-// softmax. With the scales f_j, g_j of key j's rows:
+// softmax; a list is row p of the masks of its heads. With the scales f_j, g_j of key j's rows, for each of a list's G heads
 //   z_j = (sum_d q_d kcode_jd) f_j scale log2 e,   w_j = 2^(z_j - m),   O = sum_j (w_j g_j) vcode_j / sum_j w_j.
 //
-// HBM bound: 2 d bytes per kept key. A row is read by LPR adjacent lanes (16 codes each, 8 in the grouped forms), a lane
-// keeps four keys in flight, and the arithmetic is that of the codes: a row's scale enters once per row, not per element.
-// A list is split over workgroups where the lists alone do not fill the chip, and the last workgroup of a list to finish
-// merges its splits.
+// HBM bound: 2 d bytes per listed key, half of a bf16 cache's.
+//
+// Merged lists and plans run on the matrix cores (k_decode_quant_group): the G query vectors are columns of the B operand of
+// S^T = K Q^T and, as softmax weights, of O^T += V^T P^T, in blocks of 32 keys. What counts is that a block's arithmetic stays
+// under its share of the memory's time (8 KB per wave at d = 128, eight waves per CU: some 4000 cycles): the codes become bf16
+// between LDS and the products, which is exact, and the scales enter per key: K's in the conversion (e4m3) or on the logits
+// (int8), V's on the weights.
+// A bf16 operand has 8 significant bits, and of the 32 columns at most 8 hold heads. The others hold the same heads once
+// more: columns 8 t + x what the terms before t leave of head x's weights. With bf16 queries (exact as they are) two terms
+// are 16 bits, far below half a step of the output; with fp32 queries three terms are all 24 bits, and the queries themselves
+// are split the same way, their partial logits added across the columns.
+//
+// A list per query head has one column (k_decode_quant_heads): plain ALUs, a row by 4 or 8 adjacent lanes with 16 codes each.
+//
+// Lists are split over waves, their workgroup merges them through LDS; where the lists alone do not fill the chip, over
+// several workgroups, the last of which to finish merges those.
 #include <hip/hip_bf16.h>
 #include <math.h>
 
 #include <algorithm>
 
 #include "dam_internal.h"
+#include "dam_mfma.h"
 #include "dam_quant.h"
 #include "dam_splits.h"
 
 namespace {
 using namespace dam;
 
-constexpr int kUnroll = 4;  // keys in flight per lane
+constexpr int kBlk = 32;                    // keys per block
+constexpr int kMostWaves = 8;               // of a workgroup: the LDS of a CU at d = 128
+constexpr int kMostGroups = 32;             // workgroups of a list
+
+// A wave's LDS: two slots of K rows, two of V rows, then what goes with the rows.
+template <int D>
+struct Lds {
+  static constexpr int kSlot = kBlk * D;           // bytes of the K (or V) rows of a block
+  static constexpr int kV = 2 * kSlot;
+  static constexpr int kEntries = 4 * kSlot;       // four slots of 32 list entries and their member bytes
+  static constexpr int kScales = kEntries + 1024;  // four slots of 32 words with a K scale, 32 with a V scale
+  static constexpr int kFix = kScales + 1024;      // plans: four slots of table words
+  static constexpr int kFloat = kFix + 1024;       // the block's 32 V scales (and K scales) as fp32
+  static constexpr int kMember = kFloat + 256;     // member bytes of the next block's keys, by key
+  static constexpr int kBytes = kMember + 64;
+  // at the end, in the slots: the results of the columns' terms, [term][dims / 4][head] of 16 bytes, then (reference, sum)
+  static constexpr int kPart = 8 * D * 4;
+  static constexpr int kMl = 3 * kPart;
+};
 
 struct QDecodeArgs {
   int B, Hq, Hkv, cap, shared_lists;
-  int rows_of_kv;   // lists per KV head: query heads with a list each, or 1 merged list
-  int G;            // query heads per list
-  int splits;
-  int block_shift;  // log2 of the rows that share a scale
-  int pos, n_flags; // plans
-  uint64_t flag;    // of this call (arrive_last)
+  int G;               // query heads per KV head
+  int waves, groups;   // a list is shared by `waves` waves of each of `groups` workgroups
+  int block_shift;     // log2 of the rows that share a scale
+  uint64_t flag;       // of this call (arrive_last)
   float scale;
   int64_t q_sb, q_sh, kv_sb, kv_sh, kv_ss, s_sb, s_sh, o_sb, o_sh;
+  int pos, n_flags;    // plans: position of the query row, length P of the pattern flags
 };
 
-template <int N>
-__device__ __forceinline__ void load_q(const float *p, float *v) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const float4 a = *reinterpret_cast<const float4 *>(p + i);
-    v[i] = a.x, v[i + 1] = a.y, v[i + 2] = a.z, v[i + 3] = a.w;
+// Four or sixteen bytes per lane from a 64-bit address of the lane's own to LDS address lds_at (+ IMM) + 4 or 16 * lane.
+__device__ __forceinline__ void lds_copy4_at(unsigned lds_at, uint64_t addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_at), "v"(addr) : "memory", "m0");
+}
+template <int IMM>
+__device__ __forceinline__ void lds_copy16_at(unsigned lds_at, uint64_t addr) {
+  asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off"
+               :
+               : "s"(lds_at), "n"(IMM), "v"(addr)
+               : "memory", "scc", "m0");
+}
+
+// Where the 16-byte chunk c of row r of a block lies in its LDS row: at position c ^ spread(r). Sixteen rows read at one
+// chunk, as K's operand does, and eight rows {0..3, 8..11} or {4..7, 12..15} read at two chunks 2 i and 2 i + 1, as V's does,
+// then touch every bank once.
+template <int D>
+__device__ __forceinline__ int spread(int r) {
+  return D == 128 ? ((r >> 3) & 1) << 2 | ((r >> 1) & 1) << 1 | ((r >> 2) & 1) : (r >> 2) & 3;
+}
+
+// All ones where bit `pos` of a word is clear.
+__device__ __forceinline__ unsigned unset(unsigned w, int pos) { return ~(unsigned)__builtin_amdgcn_sbfe((int)w, pos, 1); }
+
+__device__ __forceinline__ float upper16(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
+
+__device__ __forceinline__ u32x2 lds_read_tr8(const unsigned char *lds, int byte) {
+  typedef __attribute__((ext_vector_type(2))) int i32x2;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                       (__attribute__((address_space(3))) i32x2 *)(const_cast<unsigned char *>(lds + byte))));
+}
+
+// Codes 2 i and 2 i + 1 of a word, as two bf16 numbers, times a scale (e4m3 only).
+template <int FORMAT>
+__device__ __forceinline__ unsigned to_bf16(unsigned w, int i, float scale) {
+  if constexpr (FORMAT == DAM_KV_E4M3) {
+    const auto r = i ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+    return __builtin_bit_cast(unsigned, r);
+  } else {
+    return pack_bf16((float)(int8_t)(w >> (16 * i)), (float)(int8_t)(w >> (16 * i + 8)));  // (exact)
   }
 }
-template <int N>
-__device__ __forceinline__ void load_q(const __hip_bfloat16 *p, float *v) {
+
+// Eight elements of a query as an operand: term `term` of them (bf16 queries are their first term; terms from 3 on are 0).
+__device__ __forceinline__ u32x4 query_term(const __hip_bfloat16 *p, int) { return *reinterpret_cast<const u32x4 *>(p); }
+__device__ __forceinline__ u32x4 query_term(const float *p, int term) {
+  u32x4 r;
 #pragma unroll
-  for (int i = 0; i < N; i += 8) {
-    const uint4 a = *reinterpret_cast<const uint4 *>(p + i);
-    const unsigned u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[i + 2 * k] = __uint_as_float(u[k] << 16), v[i + 2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u);
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = reinterpret_cast<const float2 *>(p)[i];
+    float a = x.x, b = x.y;
+    for (int t = 0; t < term; ++t) a -= upper16(a), b -= upper16(b);
+    r[i] = term < 3 ? __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u) : 0u;
+  }
+  return r;
+}
+
+// The sum over the four lanes n, n ^ 8, n ^ 16, n ^ 24: the logits of a head's query terms.
+__device__ __forceinline__ float over_terms(float x) {
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));  // row_ror 8
+  const u32x2 sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+
+__device__ __forceinline__ void store4(float *p, const float4 &v) {
+  if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) *reinterpret_cast<float4 *>(p) = v;
+  else p[0] = v.x, p[1] = v.y, p[2] = v.z, p[3] = v.w;
+}
+__device__ __forceinline__ void store4(__hip_bfloat16 *p, const float4 &v) {
+  const unsigned lo = pack_bf16(v.x, v.y), hi = pack_bf16(v.z, v.w);
+  if ((reinterpret_cast<uintptr_t>(p) & 7) == 0) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(lo, hi);
+  } else {
+    unsigned short *u = reinterpret_cast<unsigned short *>(p);
+    u[0] = (unsigned short)lo, u[1] = (unsigned short)(lo >> 16), u[2] = (unsigned short)hi, u[3] = (unsigned short)(hi >> 16);
   }
 }
+
+// Results of one column put together: four dims of a head, unnormalised, their reference (log2 units) and sum of weights.
+struct Merged {
+  float4 o;
+  float M, L;
+  __device__ float weight(float m) const { return __builtin_amdgcn_exp2f(m - (M == -INFINITY ? 0.0f : M)); }
+  __device__ void rescale(float top) {
+    const float was = M;
+    M = top;
+    const float c = weight(was);
+    L *= c, o.x *= c, o.y *= c, o.z *= c, o.w *= c;
+  }
+  __device__ void add(float m, float l, const float4 &p) {
+    const float w = weight(m);
+    L += w * l, o.x += w * p.x, o.y += w * p.y, o.z += w * p.z, o.w += w * p.w;
+  }
+};
+
+// Groups share, share + shares, ... of a column, N fetched at a time. ml, po: the column's in group 0; strides of a group.
+template <int N>
+__device__ __forceinline__ void merge_groups(Merged &r, const float2 *ml, const float2 *po, int share, int shares, int groups,
+                                             int ml_stride, int po_stride) {
+  for (int g0 = share; g0 < groups; g0 += N * shares) {
+    float2 e[N], v[N][2];
+    float top = r.M;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int g = min(g0 + u * shares, groups - 1);
+      e[u] = load_through(ml + g * ml_stride);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) v[u][z] = load_through(po + g * po_stride + z);
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      if (g0 + u * shares >= groups) e[u] = make_float2(-INFINITY, 0.0f), v[u][0] = v[u][1] = make_float2(0.0f, 0.0f);
+      top = fmaxf(top, e[u].x);
+    }
+    r.rescale(top);
+#pragma unroll
+    for (int u = 0; u < N; ++u) r.add(e[u].x, e[u].y, make_float4(v[u][0].x, v[u][0].y, v[u][1].x, v[u][1].y));
+  }
+}
+
+// A wave owns every splits-th block of 32 list entries and two LDS slots of K and V rows, filled by load-to-LDS
+// copies whose addresses come from the list; the entries are staged three blocks ahead and the scale bytes with the rows, by
+// the same kind of copy, so that every vector-memory operation of the loop is one of these copies and the waits are counted
+// by hand. WIDE: a head's rows span 4 GiB or more, and their addresses are formed in 64 bits.
+template <typename T, int FORMAT, int D, bool PLAN, bool WIDE>
+__global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_decode_quant_group(
+    QDecodeArgs a, const T *__restrict__ q, const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
+    const uint8_t *__restrict__ ks, const uint8_t *__restrict__ vs, const int *__restrict__ kept_ptr,
+    const int *__restrict__ kept_idx, const uint8_t *__restrict__ kept_member, const uint8_t *__restrict__ plan_table,
+    float *__restrict__ part_o, float *__restrict__ part_ml, uint64_t *__restrict__ flags, T *__restrict__ out, float *__restrict__ lse) {
+  using C = Code<FORMAT>;
+  using S = Lds<D>;
+  constexpr int kTerms = sizeof(T) == 2 ? 2 : 3;  // of a weight
+  constexpr int kFrags = D / 16, kDimBlocks = D / 32;
+  constexpr int kCopies = D / 32;                 // of a block's K (or V) rows
+  constexpr bool kScaleOnLogits = FORMAT == DAM_KV_INT8;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_all[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned char *lds = lds_all + wave * S::kBytes;  // this wave's slots
+  const int n = lane & 31, hf = lane >> 5;          // column of the products, half-wave
+  const int head = n & 7, term = n >> 3;            // query head of the list, term of its weights
+  const int sub = lane / (D / 16), pos = lane % (D / 16);  // copies: row within the instruction's, 16-byte position
+  const int G = a.G;
+  const int group = (int)blockIdx.x % a.groups, pair = (int)blockIdx.x / a.groups;
+  const int splits = a.waves * a.groups, split = group * a.waves + wave;
+  const int b = pair / a.Hkv, hkv = pair % a.Hkv;
+  const int list = a.shared_lists ? hkv : pair, hq0 = hkv * G;
+  const int lo = __builtin_amdgcn_readfirstlane(kept_ptr[list]), end = __builtin_amdgcn_readfirstlane(kept_ptr[list + 1]);
+  const int n_blocks = (end - lo + kBlk - 1) / kBlk;
+  // this wave's blocks are split, split + splits, ...: every wave gets its share of each run of the list
+  const int nb = n_blocks > split ? (n_blocks - split + splits - 1) / splits : 0;
+  const float c2 = a.scale * 1.4426950408889634f;
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
+
+  f32x16 oacc[kDimBlocks];
+#pragma unroll
+  for (int db = 0; db < kDimBlocks; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) oacc[db][e] = 0.0f;
+  float m_run = -INFINITY, l_run = 0.0f;  // reference of the weights (raw logits), this lane's part of their sum
+
+  if (nb > 0) {
+    const unsigned char *kg = kc + b * a.kv_sb + hkv * a.kv_sh, *vg = vc + b * a.kv_sb + hkv * a.kv_sh;
+    const uint64_t idx_at = reinterpret_cast<uint64_t>(kept_idx), member_at = reinterpret_cast<uint64_t>(kept_member);
+    // scale bytes of K (lanes 0 .. 31) and V of this head
+    const uint64_t ks_at = reinterpret_cast<uint64_t>(ks + b * a.s_sb + hkv * a.s_sh);
+    const uint64_t vs_at = reinterpret_cast<uint64_t>(vs + b * a.s_sb + hkv * a.s_sh);
+    const uint64_t table_at = reinterpret_cast<uint64_t>(plan_table) + (uint64_t)hkv * (unsigned)a.n_flags;
+    const int last_row = PLAN ? min(a.pos, a.cap - 1) : a.cap - 1;
+    auto entry0 = [&](int i) { return lo + (split + i * splits) * kBlk; };
+    // The row of a list entry. (An index outside the cache is pulled to its nearest row; PLAN: an entry v < 0 is the diagonal
+    // -1 - v and stands for key pos + 1 + v, an entry v >= 0 is column v, and a key that does not exist yet, masked below,
+    // is taken from those that do, since rows beyond the position may hold anything.)
+    auto row_of = [&](int v) {
+      if (PLAN && v < 0) v += a.pos + 1;
+      return min(max(v, 0), last_row);
+    };
+    // Entries of local block i -> entry slot i & 3: lanes 0..31 fetch the key indices, lanes 32..40 the nine
+    // aligned words that hold the block's 32 member bytes (the other lanes repeat the ninth). Entries past the
+    // end of the list repeat its last one; their keys are masked below. An aligned word that holds a byte of
+    // an array lies inside that byte's page, so the words at the array's two ends are safe to read.
+    auto copy_entries = [&](int i) {
+      const int e0 = entry0(i);
+      const uint64_t first = (member_at + (unsigned)e0) & ~(uint64_t)3, last = (member_at + (unsigned)(end - 1)) & ~(uint64_t)3;
+      const uint64_t addr = lane < 32 ? idx_at + 4ull * (unsigned)min(e0 + n, end - 1)
+                                                        : min(first + 4u * (unsigned)min(lane - 32, 8), last);
+      lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kEntries + (i & 3) * 256), addr);
+    };
+    auto entry = [&](int i, int k) { return *reinterpret_cast<const int *>(lds + S::kEntries + (i & 3) * 256 + 4 * k); };
+    // PLAN: the aligned word that holds table[pos - c] for every column entry c of local block i (its entries have
+    // landed) -> fix slot i & 3, lane k < 32 for entry k; every other lane and entry fetches the table's first word.
+    // (A block without a column entry issues no copy: the copy, when there is one, is older than the copies of the
+    // block's scales and rows, which are all that the waits below leave outstanding.)
+    auto table_index = [&](int v) { return (v >= 0 && v <= a.pos && a.pos - v < a.n_flags) ? a.pos - v : -1; };
+    auto copy_fix = [&](int i) {
+      const int t = lane < 32 ? table_index(entry(i, lane & 31)) : -1;
+      if (__builtin_amdgcn_ballot_w64(t >= 0) == 0) return;
+      const uint64_t addr = t >= 0 ? (table_at + (unsigned)t) & ~(uint64_t)3 : reinterpret_cast<uint64_t>(plan_table) & ~(uint64_t)3;
+      lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kFix + (i & 3) * 256), addr);
+    };
+    // Scales and rows of local block i: one copy of the words that hold the 32 keys' scale bytes, kCopies of K rows and as
+    // many of V rows into slot i & 1, LDS row r for key r of the block. Returns where in those words the scale bytes of key
+    // lane & 31 lie (bits of K's, and of V's from bit 8 on).
+    auto copy_rows = [&](int i) {
+      const unsigned k_at = __builtin_amdgcn_readfirstlane(lds_base + (i & 1) * S::kSlot);
+      const unsigned v_at = k_at + S::kV;
+      const unsigned s = (unsigned)row_of(entry(i, n)) >> a.block_shift;
+      lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kScales + (i & 3) * 256), ((hf ? vs_at : ks_at) + s) & ~(uint64_t)3);
+      if constexpr (WIDE) {
+        uint64_t off[kCopies];
+#pragma unroll
+        for (int it = 0; it < kCopies; ++it) {
+          const int r = 64 / (D / 16) * it + sub;
+          off[it] = (uint64_t)row_of(entry(i, r)) * (uint64_t)a.kv_ss + ((pos ^ spread<D>(r)) << 4);
+        }
+        const uint64_t k0 = reinterpret_cast<uint64_t>(kg), v0 = reinterpret_cast<uint64_t>(vg);
+        lds_copy16_at<0 * 1024>(k_at, k0 + off[0]);
+        lds_copy16_at<1 * 1024>(k_at, k0 + off[1]);
+        if constexpr (kCopies == 4) lds_copy16_at<2 * 1024>(k_at, k0 + off[2]), lds_copy16_at<3 * 1024>(k_at, k0 + off[3]);
+        lds_copy16_at<0 * 1024>(v_at, v0 + off[0]);
+        lds_copy16_at<1 * 1024>(v_at, v0 + off[1]);
+        if constexpr (kCopies == 4) lds_copy16_at<2 * 1024>(v_at, v0 + off[2]), lds_copy16_at<3 * 1024>(v_at, v0 + off[3]);
+      } else {
+        unsigned off[kCopies];
+#pragma unroll
+        for (int it = 0; it < kCopies; ++it) {
+          const int r = 64 / (D / 16) * it + sub;
+          // (row index and row stride are below 2^24: the 24-bit multiply runs at full rate, the 32-bit one does not)
+          off[it] = __umul24((unsigned)row_of(entry(i, r)), (unsigned)a.kv_ss) + ((pos ^ spread<D>(r)) << 4);
+        }
+        lds_copy16_once<1024 * 0>(k_at, kg, off[0]);
+        lds_copy16_once<1024 * 1>(k_at, kg, off[1]);
+        if constexpr (kCopies == 4) lds_copy16_once<1024 * 2>(k_at, kg, off[2]), lds_copy16_once<1024 * 3>(k_at, kg, off[3]);
+        lds_copy16_once<1024 * 0>(v_at, vg, off[0]);
+        lds_copy16_once<1024 * 1>(v_at, vg, off[1]);
+        if constexpr (kCopies == 4) lds_copy16_once<1024 * 2>(v_at, vg, off[2]), lds_copy16_once<1024 * 3>(v_at, vg, off[3]);
+      }
+      return (((unsigned)ks_at + s) & 3) * 8 | (((unsigned)vs_at + s) & 3) * 0x800;
+    };
+    // Which heads keep which key of local block i (its entries and table words have landed): a byte per key, dealt out so
+    // that bit 8 (e % 4) of word e / 4 says whether this lane's head keeps the key of accumulator e, 8 (e / 4) + 4 hf + e % 4.
+    struct Kept {
+      unsigned w[4];
+    };
+    const int member_shift = (int)((member_at + (unsigned)lo) & 3);  // (blocks start a multiple of 32 entries apart)
+    auto keeps = [&](int i) {
+      unsigned mem = lds[S::kEntries + (i & 3) * 256 + 128 + member_shift + n];
+      if (entry0(i) + n >= end) mem = 0u;
+      if (PLAN) {
+        const int v = entry(i, n);
+        const bool exists = v < 0 ? a.pos + 1 + v >= 0 : v <= a.pos;
+        const int t = table_index(v);
+        unsigned covered = 0;  // heads that reach this column's key through a matched diagonal
+        if (t >= 0) {
+          const unsigned word = *reinterpret_cast<const unsigned *>(lds + S::kFix + (i & 3) * 256 + 4 * n);
+          covered = (word >> (8 * (int)((table_at + (unsigned)t) & 3))) & 0xFFu;
+        }
+        mem = exists ? mem & ~covered : 0u;
+      }
+      lds[S::kMember + n] = (unsigned char)mem;  // (both half-waves hold the same)
+      Kept k;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) k.w[g] = *reinterpret_cast<const unsigned *>(lds + S::kMember + 8 * g + 4 * hf) >> head;
+      return k;
+    };
+
+    // Q fragments: B operand of S^T = K Q^T. Column n is a term of query head `head` of the list (zero beyond the list's);
+    // fragment c of this lane covers dims hf D / 2 + 8 c .. + 7 (the order of the dims in the contraction is K's).
+    bf16x8 qf[kFrags];
+    {
+      const T *qp = q + b * a.q_sb + (int64_t)(hq0 + min(head, G - 1)) * a.q_sh + hf * (D / 2);
+#pragma unroll
+      for (int c = 0; c < kFrags; ++c) {
+        u32x4 raw = {0u, 0u, 0u, 0u};
+        if (head < G) raw = query_term(qp + 8 * c, term);
+        qf[c] = __builtin_bit_cast(bf16x8, raw);
+      }
+    }
+    copy_entries(0);
+    if (nb > 1) copy_entries(1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // (the Q fragments have arrived with that wait; the empty statement tells the compiler so)
+#pragma unroll
+    for (int c = 0; c < kFrags; ++c) asm volatile("" : "+v"(qf[c]));
+    if (PLAN) {
+      copy_fix(0);
+      if (nb > 1) copy_fix(1);
+    }
+    if (nb > 2) copy_entries(2);
+    unsigned bits_now = copy_rows(0), bits_next = 0;
+    if (nb > 1) bits_next = copy_rows(1);
+
+    // what a lane takes from a weight: nothing, its upper 16 bits (terms 1 and 2), and those of what remains (term 2)
+    const float less1 = term >= 1 ? 1.0f : 0.0f, less2 = term >= 2 ? 1.0f : 0.0f;
+    float *vsf = reinterpret_cast<float *>(lds + S::kFloat), *ksf = vsf + 32;
+    // LDS byte offsets of this lane's operand fragments in a slot; the others differ by an XOR (and a2 by 16 rows). K: row n,
+    // half hf of its chunks. V: a transposing read takes eight bytes of a row per lane (lanes 2 r and 2 r + 1 of sixteen the 16
+    // bytes of row r of eight) and leaves a lane the byte of its own column of all eight rows: lane n dim 32 db + n of the
+    // keys 16 a2 + 4 hf + {0..3, 8..11}, the order in which the lane holds weights.
+    const int kbase = n * D + (((D / 32 * hf) ^ spread<D>(n)) << 4);
+    const int vrow = 4 * hf + ((lane >> 1) & 3) + 8 * ((lane >> 3) & 1);
+    const int vbase = vrow * D + ((((lane >> 4) & 1) ^ spread<D>(vrow)) << 4) + 8 * (lane & 1);
+    Kept kept_now, kept_next;
+
+    for (int i = 0; i < nb; ++i) {
+      // The copies were issued in the order ... rows i, entries i + 2 (PLAN: table words i + 1), scales and rows i + 1: what
+      // block i needs and the entries of block i + 2 have landed once nothing but the copies of block i + 1's scales and rows is
+      // outstanding.
+      if (i + 1 < nb) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * kCopies + 1) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const unsigned char *kslot = lds + (i & 1) * S::kSlot;
+      const unsigned char *vslot = lds + S::kV + (i & 1) * S::kSlot;
+
+      // Everything the block needs from LDS is asked for at once, for its latency to be paid once.
+      const unsigned *words = reinterpret_cast<const unsigned *>(lds + S::kScales + (i & 3) * 256);
+      const unsigned kword = words[n], vword = words[32 + n], vfirst = vslot[n * D];
+      u32x4 kw[D / 32];
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) kw[j] = *reinterpret_cast<const u32x4 *>(kslot + (kbase ^ (j << 4)));
+      if (i == 0) kept_now = keeps(0);
+      u32x2 vw[2][kDimBlocks];
+#pragma unroll
+      for (int a2 = 0; a2 < 2; ++a2)
+#pragma unroll
+        for (int db = 0; db < kDimBlocks; ++db) vw[a2][db] = lds_read_tr8(vslot, (vbase ^ (db << 5)) + 16 * D * a2);
+
+      // Scales of key n of the block. NaN rows: the scale carries the NaN, which reaches the heads that keep the row through
+      // the logits (K's codes do so themselves in e4m3) or the weights; a V row's codes are cleared, since the product would
+      // carry them to all heads.
+      float kscale = scale_value((kword >> (bits_now & 31)) & 0xFFu);
+      float vscale = scale_value((vword >> (bits_now >> 8)) & 0xFFu);
+      const bool vbad = C::is_nan(vfirst);
+      if (vbad) vscale = NAN;
+      const unsigned vbads = (unsigned)__ballot(vbad);
+      if (kScaleOnLogits && C::is_nan(kw[0][0])) kscale = NAN;
+      if (hf == 0) {
+        vsf[n] = vscale;
+        if (kScaleOnLogits) ksf[n] = kscale;
+      }
+
+      // S^T = K Q^T; accumulator e is key 8 (e / 4) + 4 hf + e % 4
+      f32x16 s;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const u32x4 f = {to_bf16<FORMAT>(kw[j][2 * z], 0, kscale), to_bf16<FORMAT>(kw[j][2 * z], 1, kscale),
+                           to_bf16<FORMAT>(kw[j][2 * z + 1], 0, kscale), to_bf16<FORMAT>(kw[j][2 * z + 1], 1, kscale)};
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), qf[2 * j + z], s, 0, 0, 0);
+        }
+      if (i + 1 < nb) kept_next = keeps(i + 1);
+      if (kTerms == 3) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = over_terms(s[e]);
+      }
+      if (kScaleOnLogits) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 f = *reinterpret_cast<const float4 *>(ksf + 8 * g + 4 * hf);
+          s[4 * g] *= f.x, s[4 * g + 1] *= f.y, s[4 * g + 2] *= f.z, s[4 * g + 3] *= f.w;
+        }
+      }
+      // masked keys to -inf (after the products, so that a NaN row does not get past it)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const unsigned off = unset(kept_now.w[e / 4], 8 * (e % 4));
+        s[e] = __uint_as_float((off & 0xFF800000u) | (~off & __float_as_uint(s[e])));
+      }
+
+      // online softmax, one head per lane pair (lane, lane ^ 32); the reference the weights are taken against
+      // only moves when the maximum has grown past it by more than 8 in log2 units
+      float mx = s[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
+      {
+        const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      }
+      const float m_top = fmaxf(m_run, mx);
+      const bool move = (m_top - m_run) * c2 > 8.0f;  // (-inf) - (-inf) is NaN: no move
+      const float m_new = move ? m_top : m_run;
+      const float m_ref = m_new == -INFINITY ? 0.0f : m_new;
+      const float off = m_ref * c2;
+      if (__ballot(move)) {
+        const float corr = move ? __builtin_amdgcn_exp2f((m_run - m_ref) * c2) : 1.0f;  // old reference -inf: 0
+        l_run *= corr;
+#pragma unroll
+        for (int db = 0; db < kDimBlocks; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[db][e] *= corr;
+      }
+      m_run = m_new;
+      // the weights, times the scales of V's rows; the sum is taken over the weights themselves
+      float w[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -off));
+#pragma unroll
+      for (int g = 0; g < 4; ++g) l_run += (w[4 * g] + w[4 * g + 1]) + (w[4 * g + 2] + w[4 * g + 3]);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 f = *reinterpret_cast<const float4 *>(vsf + 8 * g + 4 * hf);
+        w[4 * g] *= f.x, w[4 * g + 1] *= f.y, w[4 * g + 2] *= f.z, w[4 * g + 3] *= f.w;
+      }
+      if (vbads) {  // (wave-uniform) a weight of 0 times a NaN scale; the rows' codes
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = __uint_as_float(~unset(kept_now.w[e / 4], 8 * (e % 4)) & __float_as_uint(w[e]));
+#pragma unroll
+        for (int a2 = 0; a2 < 2; ++a2)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            // bits k of the keys in bytes k of the word
+            const unsigned gone = (((vbads >> (16 * a2 + 8 * z + 4 * hf)) & 15u) * 0x204081u & 0x01010101u) * 0xFFu;
+#pragma unroll
+            for (int db = 0; db < kDimBlocks; ++db) vw[a2][db][z] &= ~gone;
+          }
+      }
+      // this lane's term of the weights
+      unsigned p[8];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        w[e] = __builtin_fmaf(-less1, upper16(w[e]), w[e]);
+        if (kTerms == 3) w[e] = __builtin_fmaf(-less2, upper16(w[e]), w[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) p[e / 2] = __builtin_amdgcn_perm(__float_as_uint(w[e + 1]), __float_as_uint(w[e]), 0x07060302u);
+
+      // O^T += V^T P^T: accumulator e of dim block db is dim 32 db + 8 (e / 4) + 4 hf + e % 4
+#pragma unroll
+      for (int a2 = 0; a2 < 2; ++a2) {
+        const u32x4 praw = {p[4 * a2], p[4 * a2 + 1], p[4 * a2 + 2], p[4 * a2 + 3]};
+#pragma unroll
+        for (int db = 0; db < kDimBlocks; ++db) {
+          const u32x2 x = vw[a2][db];
+          const u32x4 f = {to_bf16<FORMAT>(x[0], 0, 1.0f), to_bf16<FORMAT>(x[0], 1, 1.0f), to_bf16<FORMAT>(x[1], 0, 1.0f),
+                           to_bf16<FORMAT>(x[1], 1, 1.0f)};
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, praw), oacc[db],
+                                                             0, 0, 0);
+        }
+      }
+      // every LDS read of block i has returned (the products consumed them): its slots are free for block i + 2
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      kept_now = kept_next;
+      bits_now = bits_next;
+      if (i + 3 < nb) copy_entries(i + 3);
+      if (PLAN && i + 2 < nb) copy_fix(i + 2);
+      if (i + 2 < nb) bits_next = copy_rows(i + 2);
+    }
+  }
+
+  // The waves' results meet in LDS, dealt out in columns as everything from here on: column c G + x is dims 4 c .. + 3 of
+  // head x, 16 bytes at 16 (c G + x) of the wave's own slots, term t's share of it t kPart further; behind them the
+  // head's reference (log2 units) and sum.
+  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  if (head < G && term < kTerms) {
+    float4 *mine_o = reinterpret_cast<float4 *>(lds + term * S::kPart) + head;
+#pragma unroll
+    for (int db = 0; db < kDimBlocks; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        mine_o[(8 * db + 2 * g + hf) * G] =
+            make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]);
+    if (lane < 8) reinterpret_cast<float2 *>(lds + S::kMl)[n] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * c2, l_tot);
+  }
+  __syncthreads();
+  const int cols = G * (D / 4);
+  auto finish = [&](int x, int c, const float4 &o, float M, float L) {
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;  // (L = 0: no key; NaN stays)
+    store4(out + b * a.o_sb + (int64_t)(hq0 + x) * a.o_sh + 4 * c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (lse && c == 0) lse[(int64_t)b * a.Hq + hq0 + x] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  };
+  float4 *po = reinterpret_cast<float4 *>(part_o) + (int64_t)pair * a.groups * cols;  // [group][column]
+  float *ml = part_ml + (int64_t)pair * a.groups * G * 2;                             // [group][head][2]
+  for (int col = threadIdx.x; col < cols; col += blockDim.x) {
+    const int x = col % G, c = col / G;
+    Merged r = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
+    for (int w = 0; w < a.waves; ++w) r.M = fmaxf(r.M, reinterpret_cast<const float2 *>(lds_all + w * S::kBytes + S::kMl)[x].x);
+    for (int w = 0; w < a.waves; ++w) {
+      const unsigned char *its = lds_all + w * S::kBytes;
+      const float2 e = reinterpret_cast<const float2 *>(its + S::kMl)[x];
+      r.add(e.x, e.y, reinterpret_cast<const float4 *>(its)[col]);
+#pragma unroll
+      for (int t = 1; t < kTerms; ++t) r.add(e.x, 0.0f, reinterpret_cast<const float4 *>(its + t * S::kPart)[col]);
+    }
+    if (a.groups == 1) {
+      finish(x, c, r.o, r.M, r.L);
+    } else {
+      store_through(po + group * cols + col, r.o.x, r.o.y, r.o.z, r.o.w);
+      if (c == 0) {
+        store_through(ml + (group * G + x) * 2, r.M);
+        store_through(ml + (group * G + x) * 2 + 1, r.L);
+      }
+    }
+  }
+  if (a.groups == 1) return;
+  stores_done();
+  __syncthreads();
+  int *last = reinterpret_cast<int *>(lds_all + S::kEntries);  // (the results above lie below)
+  if (wave == 0) {
+    const bool is_last = arrive_last(flags + (int64_t)pair * a.groups, a.groups, group, a.flag);
+    if (lane == 0) *last = is_last;
+  }
+  __syncthreads();
+  if (!*last) return;
+  // The last workgroup merges the groups. Threads that share a column take them in turn; where there are fewer threads than
+  // columns, a thread takes several columns.
+  const int shares = max((int)blockDim.x / cols, 1), share = threadIdx.x / cols;
+  float4 *sum = reinterpret_cast<float4 *>(lds_all);  // [thread] O, then [thread] (M, L)
+  float2 *sum_ml = reinterpret_cast<float2 *>(lds_all + blockDim.x * sizeof(float4));
+  for (int col = threadIdx.x % cols; col < cols; col += blockDim.x) {
+    const int x = col % G;
+    Merged r = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
+    if (share < shares) {
+      // Bound by the latency of reading the groups back, so as many as there are, up to 16, are fetched at a time (eight heads
+      // in 32 groups: 5.2 us four at a time, 3.5 sixteen at a time), but no more: each costs a thread three loads, and sixteen
+      // for the two there are with four heads in four groups cost 2 us.
+      const int each = (a.groups + shares - 1) / shares;
+      const float2 *pm = reinterpret_cast<const float2 *>(ml) + x, *pp = reinterpret_cast<const float2 *>(po + col);
+      if (each <= 2) merge_groups<2>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
+      else if (each <= 4) merge_groups<4>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
+      else merge_groups<8>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
+    }
+    if (shares > 1) {  // (then every thread comes by here once)
+      sum[threadIdx.x] = r.o;
+      sum_ml[threadIdx.x] = make_float2(r.M, r.L);
+      __syncthreads();
+      if (share > 0) return;
+      for (int y = 1; y < shares; ++y) {
+        const float4 oy = sum[y * cols + col];
+        const float2 e = sum_ml[y * cols + col];
+        r.rescale(fmaxf(r.M, e.x));
+        r.add(e.x, e.y, oy);
+      }
+    }
+    if (share == 0) finish(x, col / G, r.o, r.M, r.L);
+  }
+}
+
+// The largest value, and the sum, over the lanes of a wave that hold the same columns (lanes LPR apart).
+template <int LPR>
+__device__ __forceinline__ float wave_max(float x) {
+  if (LPR <= 4) x = fmaxf(x, dpp_move<0x124>(x));  // row_ror 4
+  x = fmaxf(x, dpp_move<0x128>(x));                // row_ror 8
+  u32x2 sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+template <int LPR>
+__device__ __forceinline__ float row16_sum(float x) {
+  if (LPR <= 4) x += dpp_move<0x124>(x);
+  return x + dpp_move<0x128>(x);
+}
+
+// A query's sixteen elements against sixteen codes of a row.
+template <typename T, int FORMAT>
+struct Query {  // as fp32
+  float v[16];
+  __device__ void load(const float *p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = reinterpret_cast<const float4 *>(p)[i];
+      v[4 * i] = x.x, v[4 * i + 1] = x.y, v[4 * i + 2] = x.z, v[4 * i + 3] = x.w;
+    }
+  }
+  __device__ void load(const __hip_bfloat16 *p) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 x = reinterpret_cast<const u32x4 *>(p)[i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[8 * i + 2 * e] = __uint_as_float(x[e] << 16), v[8 * i + 2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+    }
+  }
+  __device__ float dot(const u32x4 &codes) const {
+    float d = 0.0f, c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      Code<FORMAT>::unpack4(codes[i], c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) d = fmaf(v[4 * i + e], c[e], d);
+    }
+    return d;
+  }
+};
+template <>
+struct Query<__hip_bfloat16, DAM_KV_E4M3> {  // pairs of bf16 numbers: products of two codes with one instruction
+  u32x4 v[2];
+  __device__ void load(const __hip_bfloat16 *p) { v[0] = reinterpret_cast<const u32x4 *>(p)[0], v[1] = reinterpret_cast<const u32x4 *>(p)[1]; }
+  __device__ float dot(const u32x4 &codes) const {
+    float d = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const unsigned x = v[i / 4][i % 4], y = to_bf16<DAM_KV_E4M3>(codes[i / 2], i % 2, 1.0f);
+      d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), d, false);
+    }
+    return d;
+  }
+};
 
 __device__ __forceinline__ void store_out(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_out(__hip_bfloat16 *p, float v) { *p = __float2bfloat16(v); }
 
-// N codes of a row as loaded.
-template <int N>
-struct Codes {
-  unsigned w[N / 4];
-  __device__ void load(const uint8_t *p) {
-    if constexpr (N == 16) {
-      const uint4 a = *reinterpret_cast<const uint4 *>(p);
-      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
-    } else {
-      const uint2 a = *reinterpret_cast<const uint2 *>(p);
-      w[0] = a.x, w[1] = a.y;
-    }
-  }
-};
-
-// The result of a list's G heads: O [head][D] unnormalised, reference (log2 units) and sum of weights. L = 0: nothing kept.
-template <typename T>
-__device__ __forceinline__ void finish(const QDecodeArgs &a, int b, int hq, int dim, float o, float M, float L, T *out,
-                                       float *lse) {
-  store_out(out + b * a.o_sb + hq * a.o_sh + dim, L == 0.0f ? 0.0f : o / L);
-  if (lse && dim == 0) lse[(int64_t)b * a.Hq + hq] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-}
-
-// GM: most query heads of a list the registers are laid out for (1: a list per query head, no member bits).
-template <typename T, int FORMAT, int D, int GM, bool PLAN>
-__global__ __launch_bounds__(256) void k_decode_quant(
+// A list per query head. A row is read by LPR adjacent lanes, and a lane keeps kUnroll keys in flight (their row numbers are
+// fetched a pass ahead); a row's scales enter once per row.
+constexpr int kUnroll = 4;
+constexpr int kHeadWaves = 8;
+constexpr int kMostHeadGroups = 16;
+template <typename T, int FORMAT, int D>
+__global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
     QDecodeArgs a, const T *__restrict__ q, const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
     const uint8_t *__restrict__ ks, const uint8_t *__restrict__ vs, const int *__restrict__ kept_ptr,
-    const int *__restrict__ kept_idx, const uint8_t *__restrict__ kept_member, const uint8_t *__restrict__ plan_table,
-    float *__restrict__ part_o, float *__restrict__ part_ml, uint64_t *__restrict__ flags, T *__restrict__ out,
-    float *__restrict__ lse) {
+    const int *__restrict__ kept_idx, float *__restrict__ part_o, float *__restrict__ part_ml, uint64_t *__restrict__ flags,
+    T *__restrict__ out, float *__restrict__ lse) {
   using C = Code<FORMAT>;
-  constexpr int N = GM == 1 ? 16 : 8;  // codes of a row per lane
-  constexpr int LPR = D / N, GROUPS = 256 / LPR;
-  __shared__ float s_o[GROUPS][D];
-  __shared__ float s_m[GROUPS], s_l[GROUPS];
+  constexpr int LPR = D / 16, GROUPS = 64 / LPR;  // lanes per row, rows of a wave
+  __shared__ float s_o[kHeadWaves][D];
+  __shared__ float2 s_ml[kHeadWaves];
   __shared__ int s_last;
 
-  // XCD-aware numbering: block n runs on XCD n % 8; all lists and splits of one (sequence, KV head) pair have ids with
-  // the same n % 8, so that heads with lists of their own find the rows they share in one L2.
-  const int per_pair = a.rows_of_kv * a.splits;
-  const int slot = (int)blockIdx.x / kXcd, pair = slot / per_pair * kXcd + (int)blockIdx.x % kXcd;
+  // block n runs on XCD n % 8: all workgroups of a (sequence, KV head) pair have ids with the same n % 8, so that its heads
+  // find the rows they share in one L2
+  const int per_pair = a.G * a.groups, slot = (int)blockIdx.x / kXcd;
+  const int pair = slot / per_pair * kXcd + (int)blockIdx.x % kXcd;
   if (pair >= a.B * a.Hkv) return;
-  const int within = slot % per_pair, nth = within / a.splits, split = within % a.splits;
   const int b = pair / a.Hkv, hkv = pair % a.Hkv;
-  const int row = hkv * a.rows_of_kv + nth;            // list of the sequence
-  const int n_rows = a.Hkv * a.rows_of_kv;
-  const int item = b * n_rows + row;
-  const int list = a.shared_lists ? row : item;
-  const int hq0 = row * a.G;                           // first query head
-  const int group = threadIdx.x / LPR, sub = threadIdx.x % LPR;
+  const int hq = hkv * a.G + slot % per_pair / a.groups, group = slot % a.groups, item = b * a.Hq + hq;
+  const int list = a.shared_lists ? hq : item;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPR;
   const int64_t end = kept_ptr[list + 1];
-  const int64_t stride = (int64_t)a.splits * GROUPS * kUnroll;
+  const int64_t stride = (int64_t)a.groups * a.waves * GROUPS * kUnroll;
 
-  float qf[GM][N];
-#pragma unroll
-  for (int x = 0; x < GM; ++x) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) qf[x][e] = 0.0f;
-    if (x < a.G) load_q<N>(q + b * a.q_sb + (hq0 + x) * a.q_sh + sub * N, qf[x]);
-  }
-  const uint8_t *kb = kc + b * a.kv_sb + hkv * a.kv_sh + sub * N, *vb = vc + b * a.kv_sb + hkv * a.kv_sh + sub * N;
+  Query<T, FORMAT> qf;
+  qf.load(q + b * a.q_sb + hq * a.q_sh + sub * 16);
+  const uint8_t *kb = kc + b * a.kv_sb + hkv * a.kv_sh + sub * 16, *vb = vc + b * a.kv_sb + hkv * a.kv_sh + sub * 16;
   const uint8_t *ksb = ks + b * a.s_sb + hkv * a.s_sh, *vsb = vs + b * a.s_sb + hkv * a.s_sh;
-  const uint8_t *table = PLAN ? plan_table + (int64_t)hkv * a.n_flags : nullptr;
   const float sl2 = a.scale * 1.4426950408889634f;  // logits in log2 units
 
-  float m[GM], l[GM], o[GM][N];
+  float m = -INFINITY, l = 0.0f, o[16];
 #pragma unroll
-  for (int x = 0; x < GM; ++x) {
-    m[x] = -INFINITY;
-    l[x] = 0.0f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) o[x][e] = 0.0f;
-  }
-
+  for (int e = 0; e < 16; ++e) o[e] = 0.0f;
   int rows[kUnroll];
-  unsigned who[kUnroll];  // member bits; 0 past the end of the list
-  int64_t p0 = kept_ptr[list] + ((int64_t)split * GROUPS + group) * kUnroll;
+  int64_t p0 = kept_ptr[list] + ((int64_t)(group * a.waves + wave) * GROUPS + lane / LPR) * kUnroll;
   auto fetch = [&](int64_t at) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const bool ok = at + u < end;
-      rows[u] = at < end ? kept_idx[ok ? at + u : at] : 0;
-      who[u] = ok ? (GM == 1 && !PLAN && !kept_member ? 1u : kept_member[at + u]) : 0u;
-    }
+    for (int u = 0; u < kUnroll; ++u) rows[u] = at < end ? kept_idx[min(at + u, end - 1)] : 0;
   };
   fetch(p0);
   for (; p0 < end; p0 += stride) {
-    Codes<N> kf[kUnroll], vf[kUnroll];
+    u32x4 kf[kUnroll], vf[kUnroll];
     float kscale[kUnroll], vscale[kUnroll];
-    unsigned cur[kUnroll], anyone = 0;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      int r = rows[u];
-      cur[u] = who[u];
-      if (PLAN) {
-        // entry -1 - r: key pos - r; entry c >= 0: key c, for the heads that do not reach it through a diagonal. A key
-        // that does not exist yet serves no head, and its row is taken from those that do.
-        const int t = a.pos - r;
-        if (r >= 0 && t >= 0 && t < a.n_flags) cur[u] &= ~(unsigned)table[t];
-        if (r < 0) r += a.pos + 1;
-        if (r < 0 || r > a.pos) cur[u] = 0;
-        r = min(max(r, 0), a.pos);
-      }
-      r = in_cache(r, a.cap);
-      kf[u].load(kb + r * a.kv_ss);
-      vf[u].load(vb + r * a.kv_ss);
+      const int r = in_cache(rows[u], a.cap);
+      kf[u] = *reinterpret_cast<const u32x4 *>(kb + r * a.kv_ss);
+      vf[u] = *reinterpret_cast<const u32x4 *>(vb + r * a.kv_ss);
       kscale[u] = scale_value(ksb[r >> a.block_shift]);
       vscale[u] = scale_value(vsb[r >> a.block_shift]);
-      anyone |= cur[u];
     }
     if (p0 + stride < end) fetch(p0 + stride);
-    // NaN rows: the scale carries the NaN, so that it reaches the heads that keep the row alone
+    float s[kUnroll], mx = m;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      if (C::is_nan(kf[u].w[0])) kscale[u] = NAN;
-      if (C::is_nan(vf[u].w[0])) {
-        vscale[u] = NAN;
+      if (C::is_nan(kf[u][0])) kscale[u] = NAN;
+      s[u] = row_sum<LPR>(qf.dot(kf[u])) * (kscale[u] * sl2);
+      if (p0 + u >= end) s[u] = -INFINITY;
+      mx = fmaxf(mx, s[u]);
+    }
+    const float ref = mx == -INFINITY ? 0.0f : mx;
+    const float corr = __builtin_amdgcn_exp2f(m - ref);
+    l *= corr;
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) vf[u].w[i] = 0u;
+    for (int e = 0; e < 16; ++e) o[e] *= corr;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const float w = __builtin_amdgcn_exp2f(s[u] - ref);
+      l += w;
+      if (C::is_nan(vf[u][0])) vscale[u] = NAN;
+      const float wv = p0 + u < end ? w * vscale[u] : 0.0f;  // (past the end: the last key once more, whatever it holds)
+      float c[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        C::unpack4(vf[u][i], c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[4 * i + e] = fmaf(wv, c[e], o[4 * i + e]);
       }
     }
-#pragma unroll
-    for (int x = 0; x < GM; ++x) {
-      if (x < a.G && __ballot((anyone >> x) & 1)) {  // some entry of this wave's pass is kept by head x
-        float s[kUnroll];
-        float mx = m[x];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          float d = 0.0f, c[4];
-#pragma unroll
-          for (int i = 0; i < N / 4; ++i) {
-            C::unpack4(kf[u].w[i], c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d = fmaf(qf[x][4 * i + e], c[e], d);
-          }
-          s[u] = (cur[u] >> x) & 1 ? row_sum<LPR>(d) * kscale[u] * sl2 : -INFINITY;
-          mx = fmaxf(mx, s[u]);
-        }
-        const float ref = mx == -INFINITY ? 0.0f : mx;  // (none of the lane's keys so far is this head's)
-        const float corr = __builtin_amdgcn_exp2f(m[x] - ref);
-        l[x] *= corr;
-#pragma unroll
-        for (int e = 0; e < N; ++e) o[x][e] *= corr;
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const float w = __builtin_amdgcn_exp2f(s[u] - ref);
-          l[x] += w;
-          const float wv = (cur[u] >> x) & 1 ? w * vscale[u] : 0.0f;
-          float c[4];
-#pragma unroll
-          for (int i = 0; i < N / 4; ++i) {
-            C::unpack4(vf[u].w[i], c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[x][4 * i + e] = fmaf(wv, c[e], o[x][4 * i + e]);
-          }
-        }
-        m[x] = mx;
-      }
-    }
+    m = mx;
   }
 
-  // the row groups of this workgroup, one head after the other through the same staging area
-  float *po = part_o + ((int64_t)item * a.splits + split) * a.G * D, *ml = part_ml + ((int64_t)item * a.splits + split) * a.G * 2;
+  // the rows of a wave, to one reference; the sums over them leave four dims to every lane of sixteen
+  const float M = wave_max<LPR>(m), ref = M == -INFINITY ? 0.0f : M, f = __builtin_amdgcn_exp2f(m - ref);
+  l = row16_sum<LPR>(l * f);
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  float t[8], r[4];
 #pragma unroll
-  for (int x = 0; x < GM; ++x) {
-    if (x < a.G) {
-      __syncthreads();
-      if (sub == 0) s_m[group] = m[x], s_l[group] = l[x];
+  for (int e = 0; e < 8; ++e) {
+    const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[e] * f), __float_as_uint(o[e + 8] * f), false, false);
+    t[e] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);  // dim e, e + 8 in the upper half-wave
+  }
 #pragma unroll
-      for (int e = 0; e < N; ++e) s_o[group][sub * N + e] = o[x][e];
-      __syncthreads();
-      if (threadIdx.x < D) {
-        float M = -INFINITY;
-        for (int g = 0; g < GROUPS; ++g) M = fmaxf(M, s_m[g]);
-        const float ref = M == -INFINITY ? 0.0f : M;
-        float L = 0.0f, acc = 0.0f;
-        for (int g = 0; g < GROUPS; ++g) {
-          const float w = __builtin_amdgcn_exp2f(s_m[g] - ref);
-          L += w * s_l[g];
-          acc += w * s_o[g][threadIdx.x];
-        }
-        if (a.splits == 1) {
-          finish(a, b, hq0 + x, threadIdx.x, acc, M, L, out, lse);
-        } else {
-          store_through(po + x * D + threadIdx.x, acc);
-          if (threadIdx.x == 0) store_through(ml + 2 * x, M), store_through(ml + 2 * x + 1, L);
-        }
-      }
+  for (int e = 0; e < 4; ++e) {
+    const u32x2 sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(t[e]), __float_as_uint(t[e + 4]), false, false);
+    r[e] = row16_sum<LPR>(__uint_as_float(sw[0]) + __uint_as_float(sw[1]));  // dim e + 4 (lane / 16)
+  }
+  if ((lane & 15) < LPR) *reinterpret_cast<float4 *>(&s_o[wave][16 * sub + 4 * (lane >> 4)]) = make_float4(r[0], r[1], r[2], r[3]);
+  if (lane == 0) s_ml[wave] = make_float2(M, l);
+  __syncthreads();
+  auto finish = [&](int dim, float acc, float top, float L) {  // (L = 0: no key)
+    store_out(out + b * a.o_sb + hq * a.o_sh + dim, L == 0.0f ? 0.0f : acc / L);
+    if (lse && dim == 0) lse[item] = L == 0.0f ? -INFINITY : (top + log2f(L)) * 0.6931471805599453f;
+  };
+  float *po = part_o + ((int64_t)item * a.groups + group) * D, *ml = part_ml + ((int64_t)item * a.groups + group) * 2;
+  for (int dim = threadIdx.x; dim < D; dim += 64 * a.waves) {
+    float top = -INFINITY, L = 0.0f, acc = 0.0f;
+    for (int w = 0; w < a.waves; ++w) top = fmaxf(top, s_ml[w].x);
+    const float to = top == -INFINITY ? 0.0f : top;
+    for (int w = 0; w < a.waves; ++w) {
+      const float x = __builtin_amdgcn_exp2f(s_ml[w].x - to);
+      L += x * s_ml[w].y;
+      acc += x * s_o[w][dim];
+    }
+    if (a.groups == 1) {
+      finish(dim, acc, top, L);
+    } else {
+      store_through(po + dim, acc);
+      if (dim == 0) store_through(ml, top), store_through(ml + 1, L);
     }
   }
-  if (a.splits == 1) return;
+  if (a.groups == 1) return;
   stores_done();
   __syncthreads();
   if (threadIdx.x < 64) {
-    const bool last = arrive_last(flags + (int64_t)item * a.splits, a.splits, split, a.flag);
+    const bool last = arrive_last(flags + (int64_t)item * a.groups, a.groups, group, a.flag);
     if (threadIdx.x == 0) s_last = last;
   }
   __syncthreads();
   if (!s_last) return;
-  // The last workgroup: a thread per pair of dims, the heads and dims in turn.
-  for (int at = threadIdx.x; at < a.G * D / 2; at += 256) {
-    const int x = at / (D / 2), c = at % (D / 2);
-    const float2 *lo = reinterpret_cast<const float2 *>(part_o + (int64_t)item * a.splits * a.G * D) + at;
-    const float2 *lm = reinterpret_cast<const float2 *>(part_ml + (int64_t)item * a.splits * a.G * 2) + x;
-    float M = -INFINITY, L = 0.0f;
+  // the last workgroup: a thread per pair of dims
+  for (int at = threadIdx.x; at < D / 2; at += 64 * a.waves) {
+    const float2 *lo = reinterpret_cast<const float2 *>(part_o + (int64_t)item * a.groups * D) + at;
+    const float2 *lm = reinterpret_cast<const float2 *>(part_ml + (int64_t)item * a.groups * 2);
+    float top = -INFINITY, L = 0.0f;
     float2 acc = make_float2(0.0f, 0.0f);
-    for (int g0 = 0; g0 < a.splits; g0 += 8) {
+    for (int g0 = 0; g0 < a.groups; g0 += 8) {
       float2 e[8], v[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int g = min(g0 + u, a.splits - 1);
-        e[u] = load_through(lm + g * a.G);
-        v[u] = load_through(lo + (int64_t)g * a.G * (D / 2));
+        const int g = min(g0 + u, a.groups - 1);
+        e[u] = load_through(lm + g);
+        v[u] = load_through(lo + g * (D / 2));
       }
-      float top = M;
+      float now = top;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        if (g0 + u >= a.splits) e[u] = make_float2(-INFINITY, 0.0f), v[u] = make_float2(0.0f, 0.0f);
-        top = fmaxf(top, e[u].x);
+        if (g0 + u >= a.groups) e[u] = make_float2(-INFINITY, 0.0f), v[u] = make_float2(0.0f, 0.0f);
+        now = fmaxf(now, e[u].x);
       }
-      const float ref = top == -INFINITY ? 0.0f : top, corr = __builtin_amdgcn_exp2f(M - ref);
+      const float to = now == -INFINITY ? 0.0f : now, corr = __builtin_amdgcn_exp2f(top - to);
       L *= corr, acc.x *= corr, acc.y *= corr;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const float w = __builtin_amdgcn_exp2f(e[u].x - ref);
+        const float w = __builtin_amdgcn_exp2f(e[u].x - to);
         L += w * e[u].y, acc.x += w * v[u].x, acc.y += w * v[u].y;
       }
-      M = top;
+      top = now;
     }
-    finish(a, b, hq0 + x, 2 * c, acc.x, M, L, out, lse);
-    finish(a, b, hq0 + x, 2 * c + 1, acc.y, M, L, out, lse);
+    finish(2 * at, acc.x, top, L);
+    finish(2 * at + 1, acc.y, top, L);
   }
 }
 
@@ -321,22 +867,45 @@ int validate_grouped(const dam_decode_params *p, const void *q, const dam_quant_
   return DAM_OK;
 }
 
-// Workgroups of a list, and the waves of each where the call takes the matrix-core kernel (`mfma`): eight waves per CU in
-// workgroups of four, each wave with at least one block of 32 entries. Up to four waves are one workgroup.
-GroupSplit splits_of(const dam_decode_params *p, int64_t max_kept, bool grouped, bool *mfma) {
+// Waves of a workgroup and workgroups of a list. Sharing a list among the waves of one workgroup is nearly free, among
+// workgroups it costs 3 to 5 us behind the loop.
+//
+// Merged lists and plans, in blocks of 32 entries: a wave per SIMD (1024) in workgroups of four as long as a wave then has no
+// more than eight blocks, which it takes at some 0.9 us each; beyond that the memory is what counts, and two waves per SIMD in
+// workgroups of eight keep more in flight (plan step at batch 16 / 64k, 13 blocks a wave: 39.7 us, with one wave per SIMD 45.0; 32
+// lists of 104 blocks: one wave per SIMD 12.9, two 13.4 to 14.1). No more workgroups than blocks need, nor than 32 a list.
+// A list per head, in passes of 32 (d = 128) or 64 keys per wave: up to eight waves of a workgroup, and as many workgroups as
+// CUs, each with a pass at least (one sequence, 32 heads, 1600 keys: 8.5 us; 15.8 in one workgroup of 16 waves per list).
+GroupSplit splits_of(const dam_decode_params *p, int64_t max_kept, bool grouped) {
   const int64_t lists = (int64_t)p->batch * (grouped ? p->hkv : p->hq);
-  *mfma = grouped && decode_quant_mfma_fits(p);
-  if (!*mfma) return {4, pick_splits(lists, max_kept)};
-  const int64_t s = std::min<int64_t>((2048 + lists - 1) / lists, std::max<int64_t>(1, max_kept / 32));
-  if (s <= 4) return {(int)s, 1};
-  const int64_t groups = std::min<int64_t>(512 / lists, max_kept / 128);
-  return {4, (int)std::min<int64_t>(std::max<int64_t>(groups, 1), 32)};
+  if (!grouped) {
+    const int per_wave = 64 / (p->head_dim / 16) * kUnroll;
+    int waves = 1;
+    while (waves < kHeadWaves && waves * per_wave < max_kept) waves *= 2;
+    return {waves, (int)std::max<int64_t>(std::min<int64_t>({256 / lists, max_kept / (waves * per_wave), (int64_t)kMostHeadGroups}), 1)};
+  }
+  const int64_t blocks = std::max<int64_t>(1, (max_kept + kBlk - 1) / kBlk);
+  const bool heavy = blocks * lists > 8 * 1024;
+  int64_t w = std::min<int64_t>(std::max<int64_t>((heavy ? 2048 : 1024) / lists, 1), blocks);
+  const int64_t rounds = (blocks + w - 1) / w;
+  w = (blocks + rounds - 1) / rounds;
+  if (w <= kMostWaves) {
+    while (heavy && (w & (w - 1))) --w;  // (workgroups of 1, 2, 4 or 8 waves share a CU without a rest)
+    return {(int)w, 1};
+  }
+  const int per = heavy ? 8 : 4;
+  return {per, (int)std::min<int64_t>({(w + per - 1) / per, 256 / lists, (int64_t)kMostGroups})};
 }
 
 // What a call writes to its workspace; lists of query heads, or of KV heads.
 Partials partials(void *ws, const dam_decode_params *p, int64_t max_kept, bool grouped) {
-  bool mfma;
-  return Partials(ws, p, splits_of(p, max_kept, grouped, &mfma).groups, (int64_t)p->batch * (grouped ? p->hkv : p->hq));
+  return Partials(ws, p, splits_of(p, max_kept, grouped).groups, (int64_t)p->batch * (grouped ? p->hkv : p->hq));
+}
+// The workspace query's: enough for every smaller bound of the lists too, which may be split into more workgroups.
+Partials most_partials(const dam_decode_params *p, int64_t max_kept, bool grouped) {
+  const int64_t lists = (int64_t)p->batch * (grouped ? p->hkv : p->hq), blocks = (max_kept + kBlk - 1) / kBlk;
+  const int64_t groups = std::min<int64_t>({(blocks + 3) / 4, 256 / lists, (int64_t)(grouped ? kMostGroups : kMostHeadGroups)});
+  return Partials(nullptr, p, (int)std::max<int64_t>(groups, 1), lists);
 }
 
 struct Plan {
@@ -350,83 +919,80 @@ struct Call {
   const dam_quant_cache *c;
   const int32_t *kept_ptr, *kept_idx;
   const uint8_t *kept_member;
+  bool grouped;
   Plan plan;
   void *out;
   float *lse;
   hipStream_t st;
 };
 
-template <typename T, int FORMAT, int D, int GM, bool PLAN>
-void launch(const Call &x, const QDecodeArgs &a, const Partials &part) {
-  const int pairs = a.B * a.Hkv, rounds = (pairs + kXcd - 1) / kXcd;
-  k_decode_quant<T, FORMAT, D, GM, PLAN><<<rounds * kXcd * a.rows_of_kv * a.splits, 256, 0, x.st>>>(
+template <typename T, int FORMAT, int D, bool PLAN, bool WIDE>
+int launch_group(const Call &x, const QDecodeArgs &a, const Partials &part) {
+  const auto kernel = k_decode_quant_group<T, FORMAT, D, PLAN, WIDE>;
+  // (more than the default limit of dynamic LDS from four waves on; idempotent, set on every call)
+  if (hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                          kMostWaves * Lds<D>::kBytes) != hipSuccess)
+    return DAM_ERR_DEVICE;
+  kernel<<<a.B * a.Hkv * a.groups, 64 * a.waves, (size_t)Lds<D>::kBytes * a.waves, x.st>>>(
       a, static_cast<const T *>(x.q), static_cast<const uint8_t *>(x.c->kcache), static_cast<const uint8_t *>(x.c->vcache),
       x.c->kscale, x.c->vscale, x.kept_ptr, x.kept_idx, x.kept_member, x.plan.table, part.o, part.ml, part.flags,
       static_cast<T *>(x.out), x.lse);
+  return launch_status();
 }
 
 template <typename T, int FORMAT, int D>
-void launch_form(const Call &x, const QDecodeArgs &a, const Partials &part) {
-  if (x.plan.table) {
-    if (a.G <= 4) launch<T, FORMAT, D, 4, true>(x, a, part);
-    else launch<T, FORMAT, D, 8, true>(x, a, part);
-  } else if (a.G == 1) {
-    launch<T, FORMAT, D, 1, false>(x, a, part);
-  } else if (a.G <= 4) {
-    launch<T, FORMAT, D, 4, false>(x, a, part);
-  } else {
-    launch<T, FORMAT, D, 8, false>(x, a, part);
+int launch_form(const Call &x, const QDecodeArgs &a, const Partials &part) {
+  if (!x.grouped) {
+    k_decode_quant_heads<T, FORMAT, D><<<(a.B * a.Hkv + kXcd - 1) / kXcd * kXcd * a.G * a.groups, 64 * a.waves, 0, x.st>>>(
+        a, static_cast<const T *>(x.q), static_cast<const uint8_t *>(x.c->kcache), static_cast<const uint8_t *>(x.c->vcache),
+        x.c->kscale, x.c->vscale, x.kept_ptr, x.kept_idx, part.o, part.ml, part.flags, static_cast<T *>(x.out), x.lse);
+    return launch_status();
   }
+  // 32-bit offsets of rows: products of a row index and a row stride of at most 24 bits each
+  const bool wide = x.p->kv_capacity >= (1 << 24) || a.kv_ss >= (1 << 24) || (uint64_t)x.p->kv_capacity * (uint64_t)a.kv_ss >= (1ull << 32);
+  if (x.plan.table)
+    return wide ? launch_group<T, FORMAT, D, true, true>(x, a, part) : launch_group<T, FORMAT, D, true, false>(x, a, part);
+  return wide ? launch_group<T, FORMAT, D, false, true>(x, a, part) : launch_group<T, FORMAT, D, false, false>(x, a, part);
+}
+
+template <typename T>
+int launch_type(const Call &x, const QDecodeArgs &a, const Partials &part) {
+  if (x.c->format == DAM_KV_E4M3)
+    return x.p->head_dim == 128 ? launch_form<T, DAM_KV_E4M3, 128>(x, a, part) : launch_form<T, DAM_KV_E4M3, 64>(x, a, part);
+  return x.p->head_dim == 128 ? launch_form<T, DAM_KV_INT8, 128>(x, a, part) : launch_form<T, DAM_KV_INT8, 64>(x, a, part);
 }
 
 // Arguments already validated, ws large enough.
-int run(const Call &x, int64_t max_kept, bool grouped, void *ws) {
+int run(const Call &x, int64_t max_kept, void *ws) {
   const dam_decode_params *p = x.p;
   QDecodeArgs a;
   a.B = p->batch; a.Hq = p->hq; a.Hkv = p->hkv; a.cap = p->kv_capacity;
   a.shared_lists = p->shared_lists != 0;
-  a.rows_of_kv = grouped ? 1 : p->hq / p->hkv;
-  a.G = grouped ? p->hq / p->hkv : 1;
-  bool mfma;
-  const GroupSplit split = splits_of(p, max_kept, grouped, &mfma);
-  a.splits = split.groups;
+  a.G = p->hq / p->hkv;
+  const GroupSplit split = splits_of(p, max_kept, x.grouped);
+  a.waves = split.waves; a.groups = split.groups;
   a.block_shift = x.c->block == 16 ? 4 : x.c->block == 32 ? 5 : x.c->block == 64 ? 6 : 7;
-  a.pos = x.plan.pos; a.n_flags = x.plan.n_flags;
+  a.flag = a.groups > 1 ? fresh_flag() : 0;
   a.scale = p->scale > 0.0f ? p->scale : 1.0f / sqrtf((float)p->head_dim);
   a.q_sb = p->q_stride[0]; a.q_sh = p->q_stride[1];
   a.kv_sb = p->kv_stride[0]; a.kv_sh = p->kv_stride[1]; a.kv_ss = p->kv_stride[2];
   a.s_sb = x.c->scale_stride[0]; a.s_sh = x.c->scale_stride[1];
   a.o_sb = p->o_stride[0]; a.o_sh = p->o_stride[1];
-  const Partials part = partials(ws, p, max_kept, grouped);
-  if (mfma)
-    return launch_decode_quant_mfma(p, split, a.scale, x.q, x.c, a.block_shift, x.kept_ptr, x.kept_idx, x.kept_member, part.o,
-                                    part.ml, part.flags, x.out, x.lse, x.st, x.plan.table, x.plan.n_flags, x.plan.pos);
-  a.flag = a.splits > 1 ? fresh_flag() : 0;
-  const bool e4m3 = x.c->format == DAM_KV_E4M3, wide = p->head_dim == 128;
-  if (p->dtype == DAM_BF16) {
-    if (e4m3 && wide) launch_form<__hip_bfloat16, DAM_KV_E4M3, 128>(x, a, part);
-    else if (e4m3) launch_form<__hip_bfloat16, DAM_KV_E4M3, 64>(x, a, part);
-    else if (wide) launch_form<__hip_bfloat16, DAM_KV_INT8, 128>(x, a, part);
-    else launch_form<__hip_bfloat16, DAM_KV_INT8, 64>(x, a, part);
-  } else {
-    if (e4m3 && wide) launch_form<float, DAM_KV_E4M3, 128>(x, a, part);
-    else if (e4m3) launch_form<float, DAM_KV_E4M3, 64>(x, a, part);
-    else if (wide) launch_form<float, DAM_KV_INT8, 128>(x, a, part);
-    else launch_form<float, DAM_KV_INT8, 64>(x, a, part);
-  }
-  return launch_status();
+  a.pos = x.plan.pos; a.n_flags = x.plan.n_flags;
+  const Partials part = partials(ws, p, max_kept, x.grouped);
+  return p->dtype == DAM_BF16 ? launch_type<__hip_bfloat16>(x, a, part) : launch_type<float>(x, a, part);
 }
 
 }  // namespace
 
 extern "C" size_t dam_sparse_attn_decode_quantized_workspace(const dam_decode_params *p, int64_t max_kept) {
   if (!p || p->batch < 1 || p->hq < 1 || p->hkv < 1 || p->hq % p->hkv || p->head_dim < 1 || max_kept < 0) return 0;
-  return bytes_up_to_batch(p, [&](const dam_decode_params *x) { return partials(nullptr, x, max_kept, false); });
+  return bytes_up_to_batch(p, [&](const dam_decode_params *x) { return most_partials(x, max_kept, false); });
 }
 
 extern "C" size_t dam_sparse_attn_decode_grouped_quantized_workspace(const dam_decode_params *p, int64_t max_kept) {
   if (!p || p->batch < 1 || p->hq < 1 || p->hkv < 1 || p->hq % p->hkv || p->head_dim < 1 || max_kept < 0) return 0;
-  return bytes_up_to_batch(p, [&](const dam_decode_params *x) { return partials(nullptr, x, max_kept, true); });
+  return bytes_up_to_batch(p, [&](const dam_decode_params *x) { return most_partials(x, max_kept, true); });
 }
 
 extern "C" int dam_sparse_attn_decode_quantized(const dam_decode_params *p, const void *q, const dam_quant_cache *cache,
@@ -435,7 +1001,7 @@ extern "C" int dam_sparse_attn_decode_quantized(const dam_decode_params *p, cons
   const int bad = validate(p, q, cache, kept_ptr, kept_idx, max_kept, out);
   if (bad != DAM_OK) return bad;
   if (!ws || ws_bytes < partials(nullptr, p, max_kept, false).bytes) return DAM_ERR_WORKSPACE;
-  return run({p, q, cache, kept_ptr, kept_idx, nullptr, {}, out, lse, static_cast<hipStream_t>(stream_v)}, max_kept, false, ws);
+  return run({p, q, cache, kept_ptr, kept_idx, nullptr, false, {}, out, lse, static_cast<hipStream_t>(stream_v)}, max_kept, ws);
 }
 
 extern "C" int dam_sparse_attn_decode_grouped_quantized(const dam_decode_params *p, const void *q, const dam_quant_cache *cache,
@@ -445,7 +1011,7 @@ extern "C" int dam_sparse_attn_decode_grouped_quantized(const dam_decode_params 
   const int bad = validate_grouped(p, q, cache, kept_ptr, kept_idx, kept_member, max_kept, out);
   if (bad != DAM_OK) return bad;
   if (!ws || ws_bytes < partials(nullptr, p, max_kept, true).bytes) return DAM_ERR_WORKSPACE;
-  return run({p, q, cache, kept_ptr, kept_idx, kept_member, {}, out, lse, static_cast<hipStream_t>(stream_v)}, max_kept, true, ws);
+  return run({p, q, cache, kept_ptr, kept_idx, kept_member, true, {}, out, lse, static_cast<hipStream_t>(stream_v)}, max_kept, ws);
 }
 
 extern "C" int dam_sparse_attn_decode_patterns_quantized(const dam_decode_params *p, const void *q,
@@ -460,6 +1026,6 @@ extern "C" int dam_sparse_attn_decode_patterns_quantized(const dam_decode_params
   dam_decode_params shared = *p;
   shared.shared_lists = 1;  // a plan belongs to the heads, not to a sequence
   if (!ws || ws_bytes < partials(nullptr, &shared, max_entries, true).bytes) return DAM_ERR_WORKSPACE;
-  return run({&shared, q, cache, plan_ptr, plan_val, plan_member, {plan_table, n_flags, pos}, out, lse,
-              static_cast<hipStream_t>(stream_v)}, max_entries, true, ws);
+  return run({&shared, q, cache, plan_ptr, plan_val, plan_member, true, {plan_table, n_flags, pos}, out, lse,
+              static_cast<hipStream_t>(stream_v)}, max_entries, ws);
 }

@@ -108,12 +108,4 @@ int launch_decode_group_mfma(const dam_decode_params *p, GroupSplit split, float
                              const uint8_t *kept_member, float *part_o, float *part_ml, uint64_t *flags, void *out,
                              float *lse, hipStream_t st, const uint8_t *plan_table = nullptr, int n_flags = 0, int pos = 0);
 
-// dam_decode_quant_mfma.hip: the same over a cache of 8-bit codes (bf16 queries, head_dim 128); block_shift is log2 of the rows
-// that share a scale.
-bool decode_quant_mfma_fits(const dam_decode_params *p);
-int launch_decode_quant_mfma(const dam_decode_params *p, GroupSplit split, float scale, const void *q, const dam_quant_cache *c,
-                             int block_shift, const int32_t *kept_ptr, const int32_t *kept_idx, const uint8_t *kept_member,
-                             float *part_o, float *part_ml, uint64_t *flags, void *out, float *lse, hipStream_t st,
-                             const uint8_t *plan_table, int n_flags, int pos);
-
 }  // namespace dam

@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "dam_internal.h"
+#include "dam_mfma.h"
 #include "dam_quant.h"
 
 namespace {
@@ -38,17 +39,93 @@ struct Span {
   }
 };
 
-// Eight elements of a row as fp32.
-__device__ __forceinline__ void load8(const float *p, float *v) {
-  const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __hip_bfloat16 *p, float *v) {
-  const uint4 a = *reinterpret_cast<const uint4 *>(p);
-  const unsigned u[4] = {a.x, a.y, a.z, a.w};
+// Eight elements of a row as read, their largest magnitude (fp32 bits) and their codes.
+template <typename T>
+struct Part;
+
+template <>
+struct Part<float> {
+  float4 v[2] = {};
+  __device__ void load(const float *p) { v[0] = reinterpret_cast<const float4 *>(p)[0], v[1] = reinterpret_cast<const float4 *>(p)[1]; }
+  __device__ void values(float (&x)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    for (int i = 0; i < 2; ++i) x[4 * i] = v[i].x, x[4 * i + 1] = v[i].y, x[4 * i + 2] = v[i].z, x[4 * i + 3] = v[i].w;
+  }
+  __device__ unsigned top() const {
+    float x[8];
+    values(x);
+    unsigned t = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+    return t;
+  }
+};
+
+template <>
+struct Part<__hip_bfloat16> {
+  u32x4 v = {0u, 0u, 0u, 0u};
+  __device__ void load(const __hip_bfloat16 *p) { v = *reinterpret_cast<const u32x4 *>(p); }
+  __device__ void values(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(v[i] << 16), x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+  }
+  __device__ unsigned top() const {
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    u16x2 t = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned m = v[i] & 0x7FFF7FFFu;
+      t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, m));
+    }
+    return (unsigned)max(t[0], t[1]) << 16;
+  }
+};
+
+// x, divided by its scale s (not 0), as codes.
+template <int FORMAT, typename T>
+__device__ __forceinline__ uint2 encode(const Part<T> &x, unsigned s) {
+  if constexpr (FORMAT == DAM_KV_E4M3 && sizeof(T) == 2) {
+    if (s < Code<FORMAT>::kHuge) {  // (the whole block) two bf16 numbers at a time, divided on the way
+      typedef __attribute__((ext_vector_type(2))) short s16x2;
+      unsigned w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned lo = x.v[2 * i], hi = x.v[2 * i + 1];
+        s16x2 r = {0, 0};
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, lo), scale_value(s), false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, hi), scale_value(s), true);
+        w[i] = __builtin_bit_cast(unsigned, r);
+      }
+      return make_uint2(w[0], w[1]);
+    }
+  }
+  float v[8];
+  x.values(v);
+  const float down = __uint_as_float((254u - s) << 23);  // 2^(127 - s)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= down;
+  return pack8<FORMAT>(v, s);
 }
+
+// The largest over the LPR adjacent lanes of a row, and over the rows of a wave from those.
+template <int CTRL>
+__device__ __forceinline__ unsigned max_with(unsigned x) {
+  return max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false));
+}
+template <int LPR>
+__device__ __forceinline__ unsigned row_max(unsigned x) {
+  x = max_with<0x141>(max_with<0x4E>(max_with<0xB1>(x)));  // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror
+  return LPR == 16 ? max_with<0x140>(x) : x;               // row_mirror
+}
+template <int LPR>
+__device__ __forceinline__ unsigned rows_max(unsigned x) {
+  if (LPR == 8) x = max_with<0x128>(x);  // row_ror 8
+  u32x2 sw = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max(sw[0], sw[1]);
+  sw = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max(sw[0], sw[1]);
+}
+
 __device__ __forceinline__ void store8(float *p, const float *v) {
   reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
   reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
@@ -81,42 +158,34 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a, const T *__res
     uint8_t *codes = (is_v ? vcache : kcache) + b * a.c_sb + h * a.c_sh + first * a.c_ss + lane8;
     uint8_t *scale = (is_v ? vscale : kscale) + b * a.s_sb + h * a.s_sh + block;
 
-    float val[PASSES][8];
+    Part<T> x_new[PASSES];
     unsigned row_top[PASSES], top = 0;  // bits of the largest magnitude: of the row, of this lane's finite rows
+    if (threadIdx.x == 0) s_top[THREADS / 64] = first < span.start ? *scale : 0u;  // (no rows in front: a new block)
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const int rel = first + p * ROWS + row0 - span.start;  // row among the new ones
-#pragma unroll
-      for (int e = 0; e < 8; ++e) val[p][e] = 0.0f;
-      if (rel >= 0 && rel < span.count) load8(x + rel * a.x_ss[is_v], val[p]);
+      if (rel >= 0 && rel < span.count) x_new[p].load(x + rel * a.x_ss[is_v]);
     }
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-      unsigned t = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(val[p][e]) & 0x7FFFFFFFu);
-      for (int off = 1; off < LPR; off <<= 1) t = max(t, (unsigned)__shfl_xor((int)t, off));
-      row_top[p] = t;
-      if (t < 0x7F800000u) top = max(top, t);
+      row_top[p] = row_max<LPR>(x_new[p].top());
+      if (row_top[p] < 0x7F800000u) top = max(top, row_top[p]);
     }
-    for (int off = LPR; off < 64; off <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, off));
+    top = rows_max<LPR>(top);
     if (threadIdx.x % 64 == 0) s_top[threadIdx.x / 64] = top;
-    if (threadIdx.x == 0) s_top[THREADS / 64] = first < span.start ? *scale : 0u;  // (no rows in front: a new block)
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) top = max(top, s_top[w]);
     const unsigned old = s_top[THREADS / 64], s = max(C::need(top), old);
-    const float down = s ? __uint_as_float((254u - s) << 23) : 0.0f;  // 2^(127 - s)
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
       const int rel = first + p * ROWS + row0 - span.start;
       uint2 *at = reinterpret_cast<uint2 *>(codes + (int64_t)(p * ROWS + row0) * a.c_ss);
       if (rel >= 0 && rel < span.count) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) val[p][e] *= down;
         const unsigned nan = C::kNan * 0x01010101u;
-        const bool bad = row_top[p] >= 0x7F800000u;
-        *at = bad ? make_uint2(nan, nan) : pack8<FORMAT>(val[p], s);
+        uint2 c = encode<FORMAT>(x_new[p], max(s, 1u));  // (s = 0: zeros, of either sign)
+        if (row_top[p] >= 0x7F800000u) c = make_uint2(nan, nan);
+        *at = c;
       } else if (rel < 0 && s > old) {  // a row in front, to the larger scale
         const uint2 was = *at;
         if (!C::is_nan(was.x)) {

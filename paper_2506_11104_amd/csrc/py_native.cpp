@@ -8,6 +8,8 @@
 // Python error of their own.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -33,6 +35,7 @@ struct Arg {
       PyErr_Format(PyExc_TypeError, "a tensor%s is wanted, got %s", maybe ? " or None" : "", Py_TYPE(o)->tp_name);
     }
   }
+  explicit Arg(const at::Tensor &x) : t(x.defined() ? &x : nullptr) {}
   void *ptr() const { return t ? t->data_ptr() : nullptr; }
   size_t bytes() const { return t ? (size_t)t->numel() : 0; }  // of a workspace: a byte tensor
   int64_t dim() const { return t->dim(); }
@@ -316,25 +319,32 @@ PyObject *kv_rows(PyObject *const *a, Py_ssize_t n) {
                : call(dam_kv_dequantize, &p, &cache.c, s, c, k.ptr(), v.ptr(), stream());
 }
 
-// The tensors and numbers of the decodes over such a cache.
+// The tensors and numbers of the decodes over such a cache. out None: made here (and lse, where it is True): two calls of
+// torch.empty cost 3.5 us in Python, about as much as the launch.
 struct QuantDecode {
-  Arg q, out, lse, ws;
+  Arg q, ws;
+  at::Tensor out, lse;
   dam_decode_params p{};
   int bad = 0;
   bool ok;
   QuantDecode(const QuantCache &cache, PyObject *q_, PyObject *out_, PyObject *lse_, PyObject *ws_, PyObject *scale_, bool shared)
-      : q(q_), out(out_), lse(lse_, true), ws(ws_, true) {
+      : q(q_), ws(ws_, true) {
     float scale;
-    ok = q.ok && out.ok && lse.ok && ws.ok && number(scale_, &scale);
+    ok = q.ok && ws.ok && number(scale_, &scale) && given(out_, out) && given(lse_ == Py_True ? Py_None : lse_, lse);
     if (!ok) return;
     p.dtype = dtype_code(q);
-    if (cache.bad || p.dtype < 0 || out.t->scalar_type() != q.t->scalar_type()) {
+    if (cache.bad || p.dtype < 0 || (out.defined() && out.scalar_type() != q.t->scalar_type())) {
       bad = cache.bad ? cache.bad : kBadDtype;
       return;
     }
-    if (q.dim() != 3 || out.t->sizes() != q.t->sizes() || q.stride(2) != 1 || out.stride(2) != 1 ||
-        q.size(0) != cache.kc.size(0) || q.size(2) != cache.kc.size(3) || !flat(lse, at::kFloat, q.size(0) * q.size(1)) ||
-        !flat(ws, at::kByte)) {
+    if (q.dim() != 3 || q.stride(2) != 1 || q.size(0) != cache.kc.size(0) || q.size(2) != cache.kc.size(3) || !flat(ws, at::kByte)) {
+      bad = kBadLayout;
+      return;
+    }
+    if (!out.defined()) out = at::empty_like(*q.t);
+    if (lse_ == Py_True) lse = at::empty({q.size(0), q.size(1)}, q.t->options().dtype(at::kFloat));
+    if (out.sizes() != q.t->sizes() || out.stride(2) != 1 ||
+        (lse.defined() && (lse.scalar_type() != at::kFloat || !lse.is_contiguous() || lse.numel() < q.size(0) * q.size(1)))) {
       bad = kBadLayout;
       return;
     }
@@ -348,7 +358,32 @@ struct QuantDecode {
     for (int i = 0; i < 3; ++i) p.kv_stride[i] = cache.kc.stride(i);
     p.shared_lists = shared ? 1 : 0;
   }
+  static bool given(PyObject *o, at::Tensor &t) {
+    const Arg a(o, true);
+    if (a.t) t = *a.t;
+    return a.ok;
+  }
+  float *lse_ptr() const { return lse.defined() ? lse.data_ptr<float>() : nullptr; }
+  // out, or (out, lse); the status where there is none
+  PyObject *result(int st) const {
+    if (st != DAM_OK) return status(st);
+    if (!lse.defined()) return THPVariable_Wrap(out);
+    PyObject *const o = THPVariable_Wrap(out), *const l = THPVariable_Wrap(lse);
+    PyObject *const both = o && l ? PyTuple_Pack(2, o, l) : nullptr;
+    Py_XDECREF(o);
+    Py_XDECREF(l);
+    return both;
+  }
 };
+
+// As call(), for the status itself.
+template <typename F, typename... A>
+int call_status(F f, A... args) {
+  PyThreadState *const saved = PyEval_SaveThread();
+  const int st = f(args...);
+  PyEval_RestoreThread(saved);
+  return st;
+}
 
 // (kcache, vcache, kscale, vscale, block, q, kept_ptr, kept_idx, kept_member, max_kept, out, lse, scale, shared, ws)
 // kept_member None: a list per query head; else merged lists per KV head.
@@ -365,14 +400,15 @@ PyObject *decode_quantized(PyObject *const *a, Py_ssize_t n) {
   if (d.bad) return status(d.bad);
   const int64_t lists = (mem.t ? d.p.hkv : d.p.hq) * (int64_t)(shared ? 1 : d.p.batch);
   if (!flat(ptr, at::kInt, lists + 1) || !flat(idx, at::kInt) || !flat(mem, at::kByte)) return status(kBadLayout);
-  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &d.q, &d.out, &d.lse, &d.ws, &ptr, &idx, &mem}))
+  const Arg out(d.out), lse(d.lse);
+  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &d.q, &out, &lse, &d.ws, &ptr, &idx, &mem}))
     return status(kBadDevice);
   const int32_t *kp = (const int32_t *)ptr.ptr(), *ki = (const int32_t *)idx.ptr();
   if (mem.t)
-    return call(dam_sparse_attn_decode_grouped_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, kp, ki, (const uint8_t *)mem.ptr(),
-                max_kept, d.out.ptr(), (float *)d.lse.ptr(), d.ws.ptr(), d.ws.bytes(), stream());
-  return call(dam_sparse_attn_decode_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, kp, ki, max_kept, d.out.ptr(),
-              (float *)d.lse.ptr(), d.ws.ptr(), d.ws.bytes(), stream());
+    return d.result(call_status(dam_sparse_attn_decode_grouped_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, kp, ki,
+                                (const uint8_t *)mem.ptr(), max_kept, out.ptr(), d.lse_ptr(), d.ws.ptr(), d.ws.bytes(), stream()));
+  return d.result(call_status(dam_sparse_attn_decode_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, kp, ki, max_kept, out.ptr(),
+                              d.lse_ptr(), d.ws.ptr(), d.ws.bytes(), stream()));
 }
 
 // (kcache, vcache, kscale, vscale, block, q, plan_ptr, plan_val, plan_member, plan_table, pos, max_entries, out, lse, scale, ws)
@@ -389,11 +425,13 @@ PyObject *decode_patterns_quantized(PyObject *const *a, Py_ssize_t n) {
   if (!flat(ptr, at::kInt, d.p.hkv + 1) || !flat(val, at::kInt) || !flat(mem, at::kByte) || !flat(tab, at::kByte) ||
       tab.dim() != 2 || tab.size(0) < d.p.hkv || pos != (int32_t)pos)
     return status(kBadLayout);
-  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &d.q, &d.out, &d.lse, &d.ws, &ptr, &val, &mem, &tab}))
+  const Arg out(d.out), lse(d.lse);
+  if (!on_current_device({&cache.kc, &cache.vc, &cache.ks, &cache.vs, &d.q, &out, &lse, &d.ws, &ptr, &val, &mem, &tab}))
     return status(kBadDevice);
-  return call(dam_sparse_attn_decode_patterns_quantized, &d.p, (const void *)d.q.ptr(), &cache.c, (const int32_t *)ptr.ptr(),
-              (const int32_t *)val.ptr(), (const uint8_t *)mem.ptr(), (const uint8_t *)tab.ptr(), (int32_t)tab.size(1), (int32_t)pos,
-              most, d.out.ptr(), (float *)d.lse.ptr(), d.ws.ptr(), d.ws.bytes(), stream());
+  return d.result(call_status(dam_sparse_attn_decode_patterns_quantized, &d.p, (const void *)d.q.ptr(), &cache.c,
+                              (const int32_t *)ptr.ptr(), (const int32_t *)val.ptr(), (const uint8_t *)mem.ptr(),
+                              (const uint8_t *)tab.ptr(), (int32_t)tab.size(1), (int32_t)pos, most, out.ptr(), d.lse_ptr(),
+                              d.ws.ptr(), d.ws.bytes(), stream()));
 }
 
 #define DAM_FN(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
