@@ -200,7 +200,8 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   constexpr int kFrags = D / 16, kDimBlocks = D / 32;
   constexpr int kCopies = D / 32;                 // of a block's K (or V) rows
   constexpr bool kScaleOnLogits = FORMAT == DAM_KV_INT8;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_all[];
+  extern __shared__ __attribute__((aligned(256))) unsigned char lds_all[];
+  __shared__ int s_last;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned char *lds = lds_all + wave * S::kBytes;  // this wave's slots
   const int n = lane & 31, hf = lane >> 5;          // column of the products, half-wave
@@ -562,13 +563,12 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   if (a.groups == 1) return;
   stores_done();
   __syncthreads();
-  int *last = reinterpret_cast<int *>(lds_all + S::kEntries);  // (the results above lie below)
   if (wave == 0) {
     const bool is_last = arrive_last(flags + (int64_t)pair * a.groups, a.groups, group, a.flag);
-    if (lane == 0) *last = is_last;
+    if (lane == 0) s_last = is_last;
   }
   __syncthreads();
-  if (!*last) return;
+  if (!s_last) return;
   // The last workgroup merges the groups. Threads that share a column take them in turn; where there are fewer threads than
   // columns, a thread takes several columns.
   const int shares = max((int)blockDim.x / cols, 1), share = threadIdx.x / cols;
@@ -1000,6 +1000,7 @@ extern "C" int dam_sparse_attn_decode_quantized(const dam_decode_params *p, cons
                                                 float *lse, void *ws, size_t ws_bytes, void *stream_v) {
   const int bad = validate(p, q, cache, kept_ptr, kept_idx, max_kept, out);
   if (bad != DAM_OK) return bad;
+  if (!aligned16(ws)) return DAM_ERR_INVALID_ARG;
   if (!ws || ws_bytes < partials(nullptr, p, max_kept, false).bytes) return DAM_ERR_WORKSPACE;
   return run({p, q, cache, kept_ptr, kept_idx, nullptr, false, {}, out, lse, static_cast<hipStream_t>(stream_v)}, max_kept, ws);
 }
@@ -1010,6 +1011,7 @@ extern "C" int dam_sparse_attn_decode_grouped_quantized(const dam_decode_params 
                                                         void *ws, size_t ws_bytes, void *stream_v) {
   const int bad = validate_grouped(p, q, cache, kept_ptr, kept_idx, kept_member, max_kept, out);
   if (bad != DAM_OK) return bad;
+  if (!aligned16(ws)) return DAM_ERR_INVALID_ARG;
   if (!ws || ws_bytes < partials(nullptr, p, max_kept, true).bytes) return DAM_ERR_WORKSPACE;
   return run({p, q, cache, kept_ptr, kept_idx, kept_member, true, {}, out, lse, static_cast<hipStream_t>(stream_v)}, max_kept, ws);
 }
@@ -1025,6 +1027,7 @@ extern "C" int dam_sparse_attn_decode_patterns_quantized(const dam_decode_params
   if (!plan_table || n_flags < 1 || pos < 0 || pos >= p->kv_capacity) return DAM_ERR_INVALID_ARG;
   dam_decode_params shared = *p;
   shared.shared_lists = 1;  // a plan belongs to the heads, not to a sequence
+  if (!aligned16(ws)) return DAM_ERR_INVALID_ARG;
   if (!ws || ws_bytes < partials(nullptr, &shared, max_entries, true).bytes) return DAM_ERR_WORKSPACE;
   return run({&shared, q, cache, plan_ptr, plan_val, plan_member, true, {plan_table, n_flags, pos}, out, lse,
               static_cast<hipStream_t>(stream_v)}, max_entries, ws);

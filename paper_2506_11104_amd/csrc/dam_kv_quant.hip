@@ -130,11 +130,8 @@ __device__ __forceinline__ void store8(float *p, const float *v) {
   reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
   reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
-__device__ __forceinline__ void store8(__hip_bfloat16 *p, const float *v) {  // (values of the cache are bf16 numbers)
-  unsigned u[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) u[i] = (__float_as_uint(v[2 * i]) >> 16) | (__float_as_uint(v[2 * i + 1]) & 0xFFFF0000u);
-  *reinterpret_cast<uint4 *>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+__device__ __forceinline__ void store8(__hip_bfloat16 *p, const float *v) {  // (exact but for values below 2^-126)
+  *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
 template <typename T, int FORMAT, int D, int BLK>

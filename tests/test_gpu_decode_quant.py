@@ -275,8 +275,84 @@ def test_a_cache_of_more_than_four_gigabytes_a_head():
     f = B.dam_sparse_attn_decode_quantized(q, small, per, i32(keys), len(keys))
     torch.cuda.synchronize()
     assert torch.equal(e, f)
-    # (beyond 4 GiB the products do not run on the matrix cores: the two agree to the rounding of the output)
-    assert ((a.float() - b.float()).abs() <= 2.0 ** -7 * b.float().abs() + 2.0 ** -14).all()
+    assert torch.equal(a, b)
+    # from a plan: 150 diagonals and twenty columns, from a position behind the border
+    pos, base = lo - lo % 128 + 299, lo - lo % 128
+    val = np.concatenate([-1 - np.arange(149, -1, -1), np.arange(20) + base])
+    table = np.zeros((1, 300), np.uint8)
+    table[0, :150] = 15
+
+    def decode(cache, at, shift):
+        v = np.where(val < 0, val, val - shift)
+        plan = B.Mask(H=4, L=0, S=300, tile_m=128, tile_n=128, kept_ptr=i32([0, len(v)]), kept_idx=i32(v),
+                      kept_member=u8([15] * len(v)), plan_table=u8(table))
+        return B.dam_sparse_attn_decode_patterns_quantized(q, cache, plan, at, len(v))
+
+    x, y = decode(c, pos, 0), decode(small, 299, base)
+    torch.cuda.synchronize()
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("fmt,dtype,d", [("e4m3", "bf16", 128), ("int8", "bf16", 64), ("e4m3", "f32", 64)])
+def test_more_blocks_than_waves_have_and_the_same_bits_twice(fmt, dtype, d):
+    """Enough long lists for workgroups of eight waves, two or more of them to a list; the second call, on another stream and
+    with another workspace, gives the same bits."""
+    rng = np.random.default_rng(52)
+    Bn, Hq, Hkv, cap = 20, 4, 2, 8000
+    c, q = make(52, fmt, dtype, Bn, Hq, Hkv, d, cap, 128)
+    common = [rng.choice(cap, 6800, replace=False) for _ in range(Hkv)]
+    lists = [[np.sort(common[h // 2][:6800 - 300 * (h % 2)]) for h in range(Hq)] for _ in range(Bn)]
+    for f in (heads, merged):
+        got = f(c, q, lists, shared=True)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            again = f(c, q, lists, shared=True)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+        pick3 = [0, 7, 19]
+        check([x[pick3] for x in got], B.QuantCache(c.k[pick3], c.v[pick3], c.kscale[pick3], c.vscale[pick3], 128) if fmt == "int8" else
+              B.QuantCache(*(x.view(torch.uint8)[pick3].view(DTYPE[fmt]) for x in (c.k, c.v)), c.kscale[pick3], c.vscale[pick3], 128),
+              fmt, q[pick3], [lists[i] for i in pick3])
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_small_configurations(seed):
+    """Sizes, layouts of heads, blocks, list lengths and positions drawn; all three forms on the same cache."""
+    rng = np.random.default_rng(1000 + seed)
+    fmt, dtype = ("e4m3", "int8")[rng.integers(2)], ("bf16", "f32")[rng.integers(2)]
+    d, block, G, Hkv, Bn = int(rng.choice([64, 128])), int(rng.choice([16, 32, 64, 128])), int(rng.integers(1, 9)), int(rng.integers(1, 4)), int(rng.integers(1, 4))
+    cap = int(rng.integers(1, 700))
+    Hq = G * Hkv
+    c, q = make(seed, fmt, dtype, Bn, Hq, Hkv, d, cap, block, spread=3.0)
+    lists = [pick(rng, cap, np.minimum(cap, rng.integers(0, 1 + cap // int(rng.integers(1, 5)), Hq))) for _ in range(Bn)]
+    scale = None if seed % 3 else 0.25
+    kw = {} if scale is None else {"scale": scale}
+    check(heads(c, q, lists, **kw), c, fmt, q, lists, scale)
+    check(merged(c, q, lists, shuffle=rng if seed % 2 else None, **kw), c, fmt, q, lists, scale)
+    P = int(rng.integers(1, cap + 50))
+    dflag, vflag = ((rng.random((Hq, P)) < rng.random() * 0.2).astype(np.uint8) for _ in range(2))
+    ptr, val, mem, table = oracle.pattern_plan(dflag, vflag, G)
+    plan = B.Mask(H=Hq, L=0, S=P, tile_m=128, tile_n=128, kept_ptr=i32(ptr), kept_idx=i32(val), kept_member=u8(mem), plan_table=u8(table))
+    pos = int(rng.integers(0, cap))
+    keep = [[np.array([j for j in range(pos + 1) if (pos - j < P and dflag[h, pos - j]) or (j < P and vflag[h, j])], np.int64)
+             for h in range(Hq)]] * Bn
+    got = B.dam_sparse_attn_decode_patterns_quantized(q, c, plan, pos, int(np.diff(ptr).max()), want_lse=True, **kw)
+    check(got, c, fmt, q, keep, scale)
+
+
+def test_outputs_that_lie_off_alignment():
+    for dtype, d, G in (("bf16", 128, 4), ("f32", 64, 2), ("bf16", 64, 1)):
+        rng = np.random.default_rng(53)
+        c, q = make(53, "e4m3", dtype, 2, 2 * G, 2, d, 300, 16)
+        lists = [pick(rng, 300, rng.integers(0, 200, 2 * G)) for _ in range(2)]
+        for f in (heads, merged):
+            want, want_lse = f(c, q, lists)
+            wide = torch.full((2, 2 * G, d + 5), 7.0, dtype=q.dtype, device="cuda")
+            got, lse = f(c, q, lists, out=wide[..., 1:d + 1])
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and torch.equal(lse, want_lse)
+            assert (wide[..., 0] == 7).all() and (wide[..., d + 1:] == 7).all()
 
 
 def test_a_decode_loop_from_a_graph():
