@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dam_internal.h"
 #include "dam_mfma.h"
@@ -673,7 +674,7 @@ __device__ __forceinline__ void store_out(__hip_bfloat16 *p, float v) { *p = __f
 constexpr int kUnroll = 4;
 constexpr int kHeadWaves = 8;
 constexpr int kMostHeadGroups = 16;
-template <typename T, int FORMAT, int D>
+template <typename T, int FORMAT, int D, bool WIDE>
 __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
     QDecodeArgs a, const T *__restrict__ q, const uint8_t *__restrict__ kc, const uint8_t *__restrict__ vc,
     const uint8_t *__restrict__ ks, const uint8_t *__restrict__ vs, const int *__restrict__ kept_ptr,
@@ -699,7 +700,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
 
   Query<T, FORMAT> qf;
   qf.load(q + b * a.q_sb + hq * a.q_sh + sub * 16);
-  const uint8_t *kb = kc + b * a.kv_sb + hkv * a.kv_sh + sub * 16, *vb = vc + b * a.kv_sb + hkv * a.kv_sh + sub * 16;
+  const uint8_t *kb = kc + b * a.kv_sb + hkv * a.kv_sh, *vb = vc + b * a.kv_sb + hkv * a.kv_sh;
   const uint8_t *ksb = ks + b * a.s_sb + hkv * a.s_sh, *vsb = vs + b * a.s_sb + hkv * a.s_sh;
   const float sl2 = a.scale * 1.4426950408889634f;  // logits in log2 units
 
@@ -718,32 +719,40 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
     float kscale[kUnroll], vscale[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int r = in_cache(rows[u], a.cap);
-      kf[u] = *reinterpret_cast<const u32x4 *>(kb + r * a.kv_ss);
-      vf[u] = *reinterpret_cast<const u32x4 *>(vb + r * a.kv_ss);
+      const unsigned r = (unsigned)in_cache(rows[u], a.cap);
+      // (a row index and a row stride below 2^24 each: the 24-bit multiply runs at full rate)
+      using Offset = std::conditional_t<WIDE, uint64_t, unsigned>;
+      const Offset at = (WIDE ? (Offset)(r * (uint64_t)a.kv_ss) : (Offset)__umul24(r, (unsigned)a.kv_ss)) + (unsigned)(16 * sub);
+      kf[u] = *reinterpret_cast<const u32x4 *>(kb + at);
+      vf[u] = *reinterpret_cast<const u32x4 *>(vb + at);
       kscale[u] = scale_value(ksb[r >> a.block_shift]);
       vscale[u] = scale_value(vsb[r >> a.block_shift]);
     }
     if (p0 + stride < end) fetch(p0 + stride);
-    float s[kUnroll], mx = m;
+    float s[kUnroll], mx = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      if (C::is_nan(kf[u][0])) kscale[u] = NAN;
+      if (FORMAT == DAM_KV_INT8 && C::is_nan(kf[u][0])) kscale[u] = NAN;  // (e4m3: the codes do it)
       s[u] = row_sum<LPR>(qf.dot(kf[u])) * (kscale[u] * sl2);
       if (p0 + u >= end) s[u] = -INFINITY;
       mx = fmaxf(mx, s[u]);
     }
-    const float ref = mx == -INFINITY ? 0.0f : mx;
-    const float corr = __builtin_amdgcn_exp2f(m - ref);
-    l *= corr;
+    // the reference of the weights moves only when the maximum has grown past it by more than 8
+    const bool move = mx > m + 8.0f;
+    if (__ballot(move)) {
+      const float to = move ? mx : m, corr = move ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
+      m = to;
+      l *= corr;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[e] *= corr;
+      for (int e = 0; e < 16; ++e) o[e] *= corr;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const float w = __builtin_amdgcn_exp2f(s[u] - ref);
       l += w;
-      if (C::is_nan(vf[u][0])) vscale[u] = NAN;
-      const float wv = p0 + u < end ? w * vscale[u] : 0.0f;  // (past the end: the last key once more, whatever it holds)
+      if (FORMAT == DAM_KV_INT8 && C::is_nan(vf[u][0])) vscale[u] = NAN;
+      const float wv = w * vscale[u];  // (past the end: the last key once more, with a weight of 0)
       float c[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -752,7 +761,6 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
         for (int e = 0; e < 4; ++e) o[4 * i + e] = fmaf(wv, c[e], o[4 * i + e]);
       }
     }
-    m = mx;
   }
 
   // the rows of a wave, to one reference; the sums over them leave four dims to every lane of sixteen
@@ -940,16 +948,19 @@ int launch_group(const Call &x, const QDecodeArgs &a, const Partials &part) {
   return launch_status();
 }
 
+template <typename T, int FORMAT, int D, bool WIDE>
+int launch_heads(const Call &x, const QDecodeArgs &a, const Partials &part) {
+  k_decode_quant_heads<T, FORMAT, D, WIDE><<<(a.B * a.Hkv + kXcd - 1) / kXcd * kXcd * a.G * a.groups, 64 * a.waves, 0, x.st>>>(
+      a, static_cast<const T *>(x.q), static_cast<const uint8_t *>(x.c->kcache), static_cast<const uint8_t *>(x.c->vcache),
+      x.c->kscale, x.c->vscale, x.kept_ptr, x.kept_idx, part.o, part.ml, part.flags, static_cast<T *>(x.out), x.lse);
+  return launch_status();
+}
+
 template <typename T, int FORMAT, int D>
 int launch_form(const Call &x, const QDecodeArgs &a, const Partials &part) {
-  if (!x.grouped) {
-    k_decode_quant_heads<T, FORMAT, D><<<(a.B * a.Hkv + kXcd - 1) / kXcd * kXcd * a.G * a.groups, 64 * a.waves, 0, x.st>>>(
-        a, static_cast<const T *>(x.q), static_cast<const uint8_t *>(x.c->kcache), static_cast<const uint8_t *>(x.c->vcache),
-        x.c->kscale, x.c->vscale, x.kept_ptr, x.kept_idx, part.o, part.ml, part.flags, static_cast<T *>(x.out), x.lse);
-    return launch_status();
-  }
   // 32-bit offsets of rows: products of a row index and a row stride of at most 24 bits each
   const bool wide = x.p->kv_capacity >= (1 << 24) || a.kv_ss >= (1 << 24) || (uint64_t)x.p->kv_capacity * (uint64_t)a.kv_ss >= (1ull << 32);
+  if (!x.grouped) return wide ? launch_heads<T, FORMAT, D, true>(x, a, part) : launch_heads<T, FORMAT, D, false>(x, a, part);
   if (x.plan.table)
     return wide ? launch_group<T, FORMAT, D, true, true>(x, a, part) : launch_group<T, FORMAT, D, true, false>(x, a, part);
   return wide ? launch_group<T, FORMAT, D, false, true>(x, a, part) : launch_group<T, FORMAT, D, false, false>(x, a, part);
