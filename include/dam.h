@@ -529,7 +529,8 @@ int dam_kv_remap_lists(const dam_evict_params *params, const int32_t *window, co
  * two's complement, -127 to 127. A row that held a value that is not finite is stored as NaN throughout (e4m3 0x7F, int8
  * -128 in every place): it takes no part in the scale of its block and reads as NaN, alone among its block's rows. A row
  * whose first code is NaN is a NaN row; the library writes no others with such codes.
- * Every value is a bf16 number, so the rows read back in bf16 or fp32 are the cache's values without another rounding.
+ * Every value is a bf16 number (but for values below 2^-126, which the decodes may take as 0), so the rows read back in
+ * bf16 or fp32 are the cache's values without another rounding.
  * ---------------------------------------------------------------------------------------------- */
 typedef enum { DAM_KV_E4M3 = 0, DAM_KV_INT8 = 1 } dam_kv_format;
 
@@ -562,10 +563,11 @@ typedef struct {
  *     s    = need where the block holds no row in front of start[b], else max(need, the block's scale so far)
  *     code = x * 2^(127 - s) rounded to nearest, ties to even;  the rows in front: code * 2^(s_old - s), the same way
  *            (where that would stand for 2^128 or more, no fp32 number any longer: the largest code below).
- * Rows in front are positions below start[b]; codes at and behind start[b] + count[b] belong to no row, are left as they
- * are and have to be written again before they are read. So a sequence is written front to back (each call continues where
- * the last one ended, or goes back to any earlier position and drops what lies behind), and the result depends on where
- * the calls' borders fall only inside the blocks that hold one.
+ * Rows in front are positions below start[b], written before (never written ones of a cache that started as zeros are zeros).
+ * Codes at and behind start[b] + count[b] belong to no row: they are left as they are, whatever their block's scale becomes,
+ * and have to be written again before they are read. So a sequence is written front to back: a call continues where the last
+ * one ended, or goes back to an earlier position and drops what lies behind. Blocks that lie within one call do not depend on
+ * where the calls' borders fall.
  * k, v     device [batch][hkv][n_rows][head_dim] by the strides.
  * start    device i32 [batch] or NULL (pos for all); count device i32 [batch] or NULL (n_rows for all; counts above n_rows
  *          or below 0 are taken as those). Device data that the host cannot check: a sequence whose start lies outside
@@ -582,9 +584,10 @@ int dam_kv_dequantize(const dam_quant_params *params, const dam_quant_cache *cac
 
 /* dam_sparse_attn_decode, _grouped and _patterns over such a cache: the same lists, plans, parameters (dtype is that of q and
  * out, bf16 or fp32; kv_stride and kv_capacity are the cache's, its rows 16-byte aligned) and results, on the cache's values.
- * Products and softmax are evaluated in fp32; where the products run on the matrix cores (bf16, head_dim 128, merged
- * lists and plans) the values are exact bf16 numbers and the softmax weights go in as two bf16 terms each (16 bits).
- * A NaN row makes the outputs of the heads that keep it NaN and no others. Plans are decoded for every dtype and head_dim.
+ * Softmax and sums are evaluated in fp32. The products of merged lists and plans run on the matrix cores, where the cache's
+ * values are exact; with bf16 queries the softmax weights go in as two bf16 terms each (16 bits), with fp32 queries the
+ * queries and the weights as three (24 bits). A NaN row makes the outputs of the heads that keep it NaN and no others. Plans
+ * are decoded for every dtype and head_dim, caches of any size in every form.
  * max_kept, the lists' bounds, clamped indices and empty lists (O = 0, lse = -inf) as for those calls. */
 size_t dam_sparse_attn_decode_quantized_workspace(const dam_decode_params *params, int64_t max_kept);
 int dam_sparse_attn_decode_quantized(const dam_decode_params *params, const void *q, const dam_quant_cache *cache,

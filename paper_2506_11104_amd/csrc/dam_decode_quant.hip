@@ -35,6 +35,8 @@
 namespace {
 using namespace dam;
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
 constexpr int kBlk = 32;                    // keys per block
 constexpr int kMostWaves = 8;               // of a workgroup: the LDS of a CU at d = 128
 constexpr int kMostGroups = 32;             // workgroups of a list
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       const int e0 = entry0(i);
       const uint64_t first = (member_at + (unsigned)e0) & ~(uint64_t)3, last = (member_at + (unsigned)(end - 1)) & ~(uint64_t)3;
       const uint64_t addr = lane < 32 ? idx_at + 4ull * (unsigned)min(e0 + n, end - 1)
-                                                        : min(first + 4u * (unsigned)min(lane - 32, 8), last);
+                                      : min(first + 4u * (unsigned)min(lane - 32, 8), last);
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kEntries + (i & 3) * 256), addr);
     };
     auto entry = [&](int i, int k) { return *reinterpret_cast<const int *>(lds + S::kEntries + (i & 3) * 256 + 4 * k); };
@@ -426,8 +428,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       if (kScaleOnLogits) {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const float4 f = *reinterpret_cast<const float4 *>(ksf + 8 * g + 4 * hf);
-          s[4 * g] *= f.x, s[4 * g + 1] *= f.y, s[4 * g + 2] *= f.z, s[4 * g + 3] *= f.w;
+          const f32x4 f = *reinterpret_cast<const f32x4 *>(ksf + 8 * g + 4 * hf);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * g + e] *= f[e];
         }
       }
       // masked keys to -inf (after the products, so that a NaN row does not get past it)
@@ -468,8 +471,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       for (int g = 0; g < 4; ++g) l_run += (w[4 * g] + w[4 * g + 1]) + (w[4 * g + 2] + w[4 * g + 3]);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 f = *reinterpret_cast<const float4 *>(vsf + 8 * g + 4 * hf);
-        w[4 * g] *= f.x, w[4 * g + 1] *= f.y, w[4 * g + 2] *= f.z, w[4 * g + 3] *= f.w;
+        const f32x4 f = *reinterpret_cast<const f32x4 *>(vsf + 8 * g + 4 * hf);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * g + e] *= f[e];
       }
       if (vbads) {  // (wave-uniform) a weight of 0 times a NaN scale; the rows' codes
 #pragma unroll
@@ -579,9 +583,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     const int x = col % G;
     Merged r = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
     if (share < shares) {
-      // Bound by the latency of reading the groups back, so as many as there are, up to 16, are fetched at a time (eight heads
-      // in 32 groups: 5.2 us four at a time, 3.5 sixteen at a time), but no more: each costs a thread three loads, and sixteen
-      // for the two there are with four heads in four groups cost 2 us.
+      // Bound by the latency of reading the groups back: as many as there are, up to eight, are fetched at a time (one sequence
+      // at 128k, eight heads in 32 groups, four at a time 15.4 us, eight 14.6), but no more: each costs a thread three loads
+      // (plan step at batch 16 / 64k, two groups for a thread, two at a time 40.4 us, eight 41.1, sixteen 42.9).
       const int each = (a.groups + shares - 1) / shares;
       const float2 *pm = reinterpret_cast<const float2 *>(ml) + x, *pp = reinterpret_cast<const float2 *>(po + col);
       if (each <= 2) merge_groups<2>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
