@@ -162,28 +162,37 @@ struct Merged {
   }
 };
 
-// Groups share, share + shares, ... of a column, N fetched at a time. ml, po: the column's in group 0; strides of a group.
+// As load_through, 16 bytes at byte `at` behind a base that is the same for the whole wave.
+__device__ __forceinline__ float4 load_through16(const void *base, unsigned at) {
+  constexpr int kSc1 = 16;             // past this XCD's L2
+  constexpr int kWords = 0x00020000;   // a resource of plain 32-bit words
+  const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, -1, kWords);
+  const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(all, at, 0, kSc1);
+  return make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
+}
+
+// Groups share, share + shares, ... of column `col` (of head x) of a list, N fetched at a time.
 template <int N>
-__device__ __forceinline__ void merge_groups(Merged &r, const float2 *ml, const float2 *po, int share, int shares, int groups,
-                                             int ml_stride, int po_stride) {
+__device__ __forceinline__ void merge_groups(Merged &r, const float *ml, const float4 *po, int share, int shares, int groups,
+                                             int col, int cols, int x, int heads) {
   for (int g0 = share; g0 < groups; g0 += N * shares) {
-    float2 e[N], v[N][2];
+    float2 e[N];
+    float4 v[N];
     float top = r.M;
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int g = min(g0 + u * shares, groups - 1);
-      e[u] = load_through(ml + g * ml_stride);
-#pragma unroll
-      for (int z = 0; z < 2; ++z) v[u][z] = load_through(po + g * po_stride + z);
+      e[u] = load_through(reinterpret_cast<const float2 *>(ml) + g * heads + x);
+      v[u] = load_through16(po, (unsigned)(g * cols + col) * 16u);
     }
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      if (g0 + u * shares >= groups) e[u] = make_float2(-INFINITY, 0.0f), v[u][0] = v[u][1] = make_float2(0.0f, 0.0f);
+      if (g0 + u * shares >= groups) e[u] = make_float2(-INFINITY, 0.0f), v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
       top = fmaxf(top, e[u].x);
     }
     r.rescale(top);
 #pragma unroll
-    for (int u = 0; u < N; ++u) r.add(e[u].x, e[u].y, make_float4(v[u][0].x, v[u][0].y, v[u][1].x, v[u][1].y));
+    for (int u = 0; u < N; ++u) r.add(e[u].x, e[u].y, v[u]);
   }
 }
 
@@ -587,10 +596,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       // at 128k, eight heads in 32 groups, four at a time 15.4 us, eight 14.6), but no more: each costs a thread three loads
       // (plan step at batch 16 / 64k, two groups for a thread, two at a time 40.4 us, eight 41.1, sixteen 42.9).
       const int each = (a.groups + shares - 1) / shares;
-      const float2 *pm = reinterpret_cast<const float2 *>(ml) + x, *pp = reinterpret_cast<const float2 *>(po + col);
-      if (each <= 2) merge_groups<2>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
-      else if (each <= 4) merge_groups<4>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
-      else merge_groups<8>(r, pm, pp, share, shares, a.groups, G, 2 * cols);
+      if (each <= 2) merge_groups<2>(r, ml, po, share, shares, a.groups, col, cols, x, G);
+      else if (each <= 4) merge_groups<4>(r, ml, po, share, shares, a.groups, col, cols, x, G);
+      else merge_groups<8>(r, ml, po, share, shares, a.groups, col, cols, x, G);
     }
     if (shares > 1) {  // (then every thread comes by here once)
       sum[threadIdx.x] = r.o;
