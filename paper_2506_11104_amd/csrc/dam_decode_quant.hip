@@ -10,12 +10,13 @@
 // Merged lists and plans run on the matrix cores (k_decode_quant_group): the G query vectors are columns of the B operand of
 // S^T = K Q^T and, as softmax weights, of O^T += V^T P^T, in blocks of 32 keys. What counts is that a block's arithmetic stays
 // under its share of the memory's time (8 KB per wave at d = 128, eight waves per CU: some 4000 cycles): the codes become bf16
-// between LDS and the products, which is exact, and the scales enter per key: K's in the conversion (e4m3) or on the logits
-// (int8), V's on the weights.
-// A bf16 operand has 8 significant bits, and of the 32 columns at most 8 hold heads. The others hold the same heads once
+// between LDS and the products, which is exact, and the scales enter per key: K's on the logits, V's on the weights.
+// A bf16 operand has 8 significant bits, and of a tile's 16 columns at most 8 hold heads. The others hold the same heads once
 // more: columns 8 t + x what the terms before t leave of head x's weights. With bf16 queries (exact as they are) two terms
-// are 16 bits, far below half a step of the output; with fp32 queries three terms are all 24 bits, and the queries themselves
-// are split the same way, their partial logits added across the columns.
+// are 16 bits, far below half a step of the output; with fp32 queries three terms are all 24 bits, in two tiles of columns, and
+// the queries themselves are split the same way, their partial logits added across the columns. (In products of 32 x 32, half
+// of whose columns were idle, a lane had twice the logits to take through the softmax: plan step at batch 16 / 64k 39.7 us,
+// now 38.8; fp32, two sequences at 32k 16.4, now 14.5; a block alone some 0.9 us, now 0.8.)
 //
 // A list per query head has one column (k_decode_quant_heads): plain ALUs, a row by 4 or 8 adjacent lanes with 16 codes each.
 //
@@ -80,13 +81,15 @@ __device__ __forceinline__ void lds_copy16_at(unsigned lds_at, uint64_t addr) {
                : "memory", "scc", "m0");
 }
 
-// Where the 16-byte chunk c of row r of a block lies in its LDS row: at position c ^ spread(r). Sixteen rows read at one
-// chunk, as K's operand does, and eight rows {0..3, 8..11} or {4..7, 12..15} read at two chunks 2 i and 2 i + 1, as V's does,
-// then touch every bank once.
+// Where the 16-byte chunk c of row r of a block lies in its LDS row: at position c ^ spread(r). Sixteen rows 16 t .. read at one
+// chunk, as K's operand does, and the sixteen rows {0..7, 16..23} or {8..15, 24..31}, as V's does, then touch every bank once.
 template <int D>
 __device__ __forceinline__ int spread(int r) {
-  return D == 128 ? ((r >> 3) & 1) << 2 | ((r >> 1) & 1) << 1 | ((r >> 2) & 1) : (r >> 2) & 3;
+  const int top = ((r >> 3) ^ (r >> 4)) & 1;
+  return D == 128 ? top << 2 | ((r >> 1) & 3) : top << 1 | ((r >> 2) & 1);
 }
+
+constexpr int spread_of_16(int d) { return d == 128 ? 4 : 2; }
 
 // All ones where bit `pos` of a word is clear.
 __device__ __forceinline__ unsigned unset(unsigned w, int pos) { return ~(unsigned)__builtin_amdgcn_sbfe((int)w, pos, 1); }
@@ -99,14 +102,14 @@ __device__ __forceinline__ u32x2 lds_read_tr8(const unsigned char *lds, int byte
                                        (__attribute__((address_space(3))) i32x2 *)(const_cast<unsigned char *>(lds + byte))));
 }
 
-// Codes 2 i and 2 i + 1 of a word, as two bf16 numbers, times a scale (e4m3 only).
+// Codes 2 i and 2 i + 1 of a word, as two bf16 numbers (exact).
 template <int FORMAT>
-__device__ __forceinline__ unsigned to_bf16(unsigned w, int i, float scale) {
+__device__ __forceinline__ unsigned to_bf16(unsigned w, int i) {
   if constexpr (FORMAT == DAM_KV_E4M3) {
-    const auto r = i ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
+    const auto r = i ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
     return __builtin_bit_cast(unsigned, r);
   } else {
-    return pack_bf16((float)(int8_t)(w >> (16 * i)), (float)(int8_t)(w >> (16 * i + 8)));  // (exact)
+    return pack_bf16((float)(int8_t)(w >> (16 * i)), (float)(int8_t)(w >> (16 * i + 8)));
   }
 }
 
@@ -124,11 +127,12 @@ __device__ __forceinline__ u32x4 query_term(const float *p, int term) {
   return r;
 }
 
-// The sum over the four lanes n, n ^ 8, n ^ 16, n ^ 24: the logits of a head's query terms.
-__device__ __forceinline__ float over_terms(float x) {
-  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xF, 0xF, false));  // row_ror 8
-  const u32x2 sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+// The largest over the four lanes that hold a column's keys.
+__device__ __forceinline__ float column_max(float x) {
+  u32x2 sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
 }
 
 __device__ __forceinline__ void store4(float *p, const float4 &v) {
@@ -209,15 +213,17 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   using C = Code<FORMAT>;
   using S = Lds<D>;
   constexpr int kTerms = sizeof(T) == 2 ? 2 : 3;  // of a weight
-  constexpr int kFrags = D / 16, kDimBlocks = D / 32;
+  constexpr int kTiles = (kTerms + 1) / 2;        // of 16 columns: two terms of eight heads
+  constexpr int kFrags = D / 32;                  // of a key's dims, a quarter of them per lane
+  constexpr int kDims = D / 16;                   // blocks of 16 dims
   constexpr int kCopies = D / 32;                 // of a block's K (or V) rows
-  constexpr bool kScaleOnLogits = FORMAT == DAM_KV_INT8;
   extern __shared__ __attribute__((aligned(256))) unsigned char lds_all[];
   __shared__ int s_last;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned char *lds = lds_all + wave * S::kBytes;  // this wave's slots
-  const int n = lane & 31, hf = lane >> 5;          // column of the products, half-wave
-  const int head = n & 7, term = n >> 3;            // query head of the list, term of its weights
+  const int n = lane & 15, kg = lane >> 4;          // column of the products, quarter of the wave
+  const int head = n & 7, term = n >> 3;            // query head of the list, term of its weights (in the first tile)
+  const int key = lane & 31, hf = lane >> 5;        // where a lane stands for a key of the block
   const int sub = lane / (D / 16), pos = lane % (D / 16);  // copies: row within the instruction's, 16-byte position
   const int G = a.G;
   const int group = (int)blockIdx.x % a.groups, pair = (int)blockIdx.x / a.groups;
@@ -231,15 +237,15 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   const float c2 = a.scale * 1.4426950408889634f;
   const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds;
 
-  f32x16 oacc[kDimBlocks];
+  f32x4 oacc[kTiles][kDims];
 #pragma unroll
-  for (int db = 0; db < kDimBlocks; ++db)
+  for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) oacc[db][e] = 0.0f;
+    for (int dt = 0; dt < kDims; ++dt) oacc[j][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m_run = -INFINITY, l_run = 0.0f;  // reference of the weights (raw logits), this lane's part of their sum
 
   if (nb > 0) {
-    const unsigned char *kg = kc + b * a.kv_sb + hkv * a.kv_sh, *vg = vc + b * a.kv_sb + hkv * a.kv_sh;
+    const unsigned char *k_rows = kc + b * a.kv_sb + hkv * a.kv_sh, *v_rows = vc + b * a.kv_sb + hkv * a.kv_sh;
     const uint64_t idx_at = reinterpret_cast<uint64_t>(kept_idx), member_at = reinterpret_cast<uint64_t>(kept_member);
     // scale bytes of K (lanes 0 .. 31) and V of this head
     const uint64_t ks_at = reinterpret_cast<uint64_t>(ks + b * a.s_sb + hkv * a.s_sh);
@@ -261,7 +267,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     auto copy_entries = [&](int i) {
       const int e0 = entry0(i);
       const uint64_t first = (member_at + (unsigned)e0) & ~(uint64_t)3, last = (member_at + (unsigned)(end - 1)) & ~(uint64_t)3;
-      const uint64_t addr = lane < 32 ? idx_at + 4ull * (unsigned)min(e0 + n, end - 1)
+      const uint64_t addr = lane < 32 ? idx_at + 4ull * (unsigned)min(e0 + key, end - 1)
                                       : min(first + 4u * (unsigned)min(lane - 32, 8), last);
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kEntries + (i & 3) * 256), addr);
     };
@@ -272,18 +278,18 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     // block's scales and rows, which are all that the waits below leave outstanding.)
     auto table_index = [&](int v) { return (v >= 0 && v <= a.pos && a.pos - v < a.n_flags) ? a.pos - v : -1; };
     auto copy_fix = [&](int i) {
-      const int t = lane < 32 ? table_index(entry(i, lane & 31)) : -1;
+      const int t = lane < 32 ? table_index(entry(i, key)) : -1;
       if (__builtin_amdgcn_ballot_w64(t >= 0) == 0) return;
       const uint64_t addr = t >= 0 ? (table_at + (unsigned)t) & ~(uint64_t)3 : reinterpret_cast<uint64_t>(plan_table) & ~(uint64_t)3;
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kFix + (i & 3) * 256), addr);
     };
     // Scales and rows of local block i: one copy of the words that hold the 32 keys' scale bytes, kCopies of K rows and as
-    // many of V rows into slot i & 1, LDS row r for key r of the block. Returns where in those words the scale bytes of key
-    // lane & 31 lie (bits of K's, and of V's from bit 8 on).
+    // many of V rows into slot i & 1, LDS row r for key r of the block. Returns where in those words the scale bytes of this
+    // lane's key lie (bits of K's, and of V's from bit 8 on).
     auto copy_rows = [&](int i) {
       const unsigned k_at = __builtin_amdgcn_readfirstlane(lds_base + (i & 1) * S::kSlot);
       const unsigned v_at = k_at + S::kV;
-      const unsigned s = (unsigned)row_of(entry(i, n)) >> a.block_shift;
+      const unsigned s = (unsigned)row_of(entry(i, key)) >> a.block_shift;
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kScales + (i & 3) * 256), ((hf ? vs_at : ks_at) + s) & ~(uint64_t)3);
       if constexpr (WIDE) {
         uint64_t off[kCopies];
@@ -292,7 +298,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
           const int r = 64 / (D / 16) * it + sub;
           off[it] = (uint64_t)row_of(entry(i, r)) * (uint64_t)a.kv_ss + ((pos ^ spread<D>(r)) << 4);
         }
-        const uint64_t k0 = reinterpret_cast<uint64_t>(kg), v0 = reinterpret_cast<uint64_t>(vg);
+        const uint64_t k0 = reinterpret_cast<uint64_t>(k_rows), v0 = reinterpret_cast<uint64_t>(v_rows);
         lds_copy16_at<0 * 1024>(k_at, k0 + off[0]);
         lds_copy16_at<1 * 1024>(k_at, k0 + off[1]);
         if constexpr (kCopies == 4) lds_copy16_at<2 * 1024>(k_at, k0 + off[2]), lds_copy16_at<3 * 1024>(k_at, k0 + off[3]);
@@ -307,60 +313,64 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
           // (row index and row stride are below 2^24: the 24-bit multiply runs at full rate, the 32-bit one does not)
           off[it] = __umul24((unsigned)row_of(entry(i, r)), (unsigned)a.kv_ss) + ((pos ^ spread<D>(r)) << 4);
         }
-        lds_copy16_once<1024 * 0>(k_at, kg, off[0]);
-        lds_copy16_once<1024 * 1>(k_at, kg, off[1]);
-        if constexpr (kCopies == 4) lds_copy16_once<1024 * 2>(k_at, kg, off[2]), lds_copy16_once<1024 * 3>(k_at, kg, off[3]);
-        lds_copy16_once<1024 * 0>(v_at, vg, off[0]);
-        lds_copy16_once<1024 * 1>(v_at, vg, off[1]);
-        if constexpr (kCopies == 4) lds_copy16_once<1024 * 2>(v_at, vg, off[2]), lds_copy16_once<1024 * 3>(v_at, vg, off[3]);
+        lds_copy16_once<1024 * 0>(k_at, k_rows, off[0]);
+        lds_copy16_once<1024 * 1>(k_at, k_rows, off[1]);
+        if constexpr (kCopies == 4) lds_copy16_once<1024 * 2>(k_at, k_rows, off[2]), lds_copy16_once<1024 * 3>(k_at, k_rows, off[3]);
+        lds_copy16_once<1024 * 0>(v_at, v_rows, off[0]);
+        lds_copy16_once<1024 * 1>(v_at, v_rows, off[1]);
+        if constexpr (kCopies == 4) lds_copy16_once<1024 * 2>(v_at, v_rows, off[2]), lds_copy16_once<1024 * 3>(v_at, v_rows, off[3]);
       }
       return (((unsigned)ks_at + s) & 3) * 8 | (((unsigned)vs_at + s) & 3) * 0x800;
     };
     // Which heads keep which key of local block i (its entries and table words have landed): a byte per key, dealt out so
-    // that bit 8 (e % 4) of word e / 4 says whether this lane's head keeps the key of accumulator e, 8 (e / 4) + 4 hf + e % 4.
+    // that bit 8 r of word t says whether this lane's head keeps the key of accumulator r of tile t, 16 t + 4 kg + r.
     struct Kept {
-      unsigned w[4];
+      unsigned w[2];
     };
     const int member_shift = (int)((member_at + (unsigned)lo) & 3);  // (blocks start a multiple of 32 entries apart)
     auto keeps = [&](int i) {
-      unsigned mem = lds[S::kEntries + (i & 3) * 256 + 128 + member_shift + n];
-      if (entry0(i) + n >= end) mem = 0u;
+      unsigned mem = lds[S::kEntries + (i & 3) * 256 + 128 + member_shift + key];
+      if (entry0(i) + key >= end) mem = 0u;
       if (PLAN) {
-        const int v = entry(i, n);
+        const int v = entry(i, key);
         const bool exists = v < 0 ? a.pos + 1 + v >= 0 : v <= a.pos;
         const int t = table_index(v);
         unsigned covered = 0;  // heads that reach this column's key through a matched diagonal
         if (t >= 0) {
-          const unsigned word = *reinterpret_cast<const unsigned *>(lds + S::kFix + (i & 3) * 256 + 4 * n);
+          const unsigned word = *reinterpret_cast<const unsigned *>(lds + S::kFix + (i & 3) * 256 + 4 * key);
           covered = (word >> (8 * (int)((table_at + (unsigned)t) & 3))) & 0xFFu;
         }
         mem = exists ? mem & ~covered : 0u;
       }
-      lds[S::kMember + n] = (unsigned char)mem;  // (both half-waves hold the same)
+      lds[S::kMember + key] = (unsigned char)mem;  // (both half-waves hold the same)
       Kept k;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) k.w[g] = *reinterpret_cast<const unsigned *>(lds + S::kMember + 8 * g + 4 * hf) >> head;
+      for (int t = 0; t < 2; ++t) k.w[t] = *reinterpret_cast<const unsigned *>(lds + S::kMember + 16 * t + 4 * kg) >> head;
       return k;
     };
 
-    // Q fragments: B operand of S^T = K Q^T. Column n is a term of query head `head` of the list (zero beyond the list's);
-    // fragment c of this lane covers dims hf D / 2 + 8 c .. + 7 (the order of the dims in the contraction is K's).
-    bf16x8 qf[kFrags];
+    // Q fragments: B operand of S^T = K Q^T. Column n of tile j is term 2 j + n / 8 of query head n % 8 of the list (zero beyond
+    // the list's); fragment c of this lane covers dims kg D / 4 + 8 c .. + 7 (the order of the dims in the contraction is K's).
+    bf16x8 qf[kTiles][kFrags];
     {
-      const T *qp = q + b * a.q_sb + (int64_t)(hq0 + min(head, G - 1)) * a.q_sh + hf * (D / 2);
+      const T *qp = q + b * a.q_sb + (int64_t)(hq0 + min(head, G - 1)) * a.q_sh + kg * (D / 4);
 #pragma unroll
-      for (int c = 0; c < kFrags; ++c) {
-        u32x4 raw = {0u, 0u, 0u, 0u};
-        if (head < G) raw = query_term(qp + 8 * c, term);
-        qf[c] = __builtin_bit_cast(bf16x8, raw);
-      }
+      for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+        for (int c = 0; c < kFrags; ++c) {
+          u32x4 raw = {0u, 0u, 0u, 0u};
+          if (head < G) raw = query_term(qp + 8 * c, 2 * j + term);
+          qf[j][c] = __builtin_bit_cast(bf16x8, raw);
+        }
     }
     copy_entries(0);
     if (nb > 1) copy_entries(1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // (the Q fragments have arrived with that wait; the empty statement tells the compiler so)
 #pragma unroll
-    for (int c = 0; c < kFrags; ++c) asm volatile("" : "+v"(qf[c]));
+    for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+      for (int c = 0; c < kFrags; ++c) asm volatile("" : "+v"(qf[j][c]));
     if (PLAN) {
       copy_fix(0);
       if (nb > 1) copy_fix(1);
@@ -369,16 +379,16 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     unsigned bits_now = copy_rows(0), bits_next = 0;
     if (nb > 1) bits_next = copy_rows(1);
 
-    // what a lane takes from a weight: nothing, its upper 16 bits (terms 1 and 2), and those of what remains (term 2)
-    const float less1 = term >= 1 ? 1.0f : 0.0f, less2 = term >= 2 ? 1.0f : 0.0f;
+    const float less = term ? 1.0f : 0.0f;  // the second term of a weight: less its upper 16 bits
     float *vsf = reinterpret_cast<float *>(lds + S::kFloat), *ksf = vsf + 32;
-    // LDS byte offsets of this lane's operand fragments in a slot; the others differ by an XOR (and a2 by 16 rows). K: row n,
-    // half hf of its chunks. V: a transposing read takes eight bytes of a row per lane (lanes 2 r and 2 r + 1 of sixteen the 16
-    // bytes of row r of eight) and leaves a lane the byte of its own column of all eight rows: lane n dim 32 db + n of the
-    // keys 16 a2 + 4 hf + {0..3, 8..11}, the order in which the lane holds weights.
-    const int kbase = n * D + (((D / 32 * hf) ^ spread<D>(n)) << 4);
-    const int vrow = 4 * hf + ((lane >> 1) & 3) + 8 * ((lane >> 3) & 1);
-    const int vbase = vrow * D + ((((lane >> 4) & 1) ^ spread<D>(vrow)) << 4) + 8 * (lane & 1);
+    // LDS byte offsets of this lane's operand fragments in a slot; the others differ by an XOR (and tile 1 by 16 rows). K: rows n
+    // and 16 + n, quarter kg of their chunks. V: a transposing read takes eight bytes of a row per lane (lanes 2 r and 2 r + 1 of
+    // sixteen the 16 bytes of row r of eight) and leaves a lane the byte of its own column of all eight rows: dim 16 dt + n of
+    // the keys 4 kg + {0..3, 16..19}, the order in which the lane holds weights.
+    constexpr int kFlip = spread_of_16(D);  // spread(r + 16) is spread(r) ^ this
+    const int kbase = n * D + (((D / 64 * kg) ^ spread<D>(n)) << 4);
+    const int vrow = 16 * ((lane >> 3) & 1) + 4 * kg + ((lane >> 1) & 3);
+    const int vbase = vrow * D + (spread<D>(vrow) << 4) + 8 * (lane & 1);
     Kept kept_now, kept_next;
 
     for (int i = 0; i < nb; ++i) {
@@ -392,73 +402,69 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
 
       // Everything the block needs from LDS is asked for at once, for its latency to be paid once.
       const unsigned *words = reinterpret_cast<const unsigned *>(lds + S::kScales + (i & 3) * 256);
-      const unsigned kword = words[n], vword = words[32 + n], vfirst = vslot[n * D];
-      u32x4 kw[D / 32];
+      const unsigned kword = words[key], vword = words[32 + key], kfirst = kslot[key * D], vfirst = vslot[key * D];
+      u32x4 kw[2][D / 64];
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) kw[j] = *reinterpret_cast<const u32x4 *>(kslot + (kbase ^ (j << 4)));
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j)
+          kw[t][j] = *reinterpret_cast<const u32x4 *>(kslot + ((kbase ^ ((j ^ (t * kFlip)) << 4)) + 16 * D * t));
       if (i == 0) kept_now = keeps(0);
-      u32x2 vw[2][kDimBlocks];
+      u32x2 vw[kDims];
 #pragma unroll
-      for (int a2 = 0; a2 < 2; ++a2)
-#pragma unroll
-        for (int db = 0; db < kDimBlocks; ++db) vw[a2][db] = lds_read_tr8(vslot, (vbase ^ (db << 5)) + 16 * D * a2);
+      for (int dt = 0; dt < kDims; ++dt) vw[dt] = lds_read_tr8(vslot, vbase ^ (dt << 4));
 
-      // Scales of key n of the block. NaN rows: the scale carries the NaN, which reaches the heads that keep the row through
-      // the logits (K's codes do so themselves in e4m3) or the weights; a V row's codes are cleared, since the product would
-      // carry them to all heads.
+      // Scales of this lane's key of the block. NaN rows: the scale carries the NaN, which reaches the heads that keep the row
+      // through the logits (K's codes do so themselves in e4m3) or the weights; a V row's codes are cleared, since the product
+      // would carry them to all heads.
       float kscale = scale_value((kword >> (bits_now & 31)) & 0xFFu);
       float vscale = scale_value((vword >> (bits_now >> 8)) & 0xFFu);
       const bool vbad = C::is_nan(vfirst);
       if (vbad) vscale = NAN;
+      if (FORMAT == DAM_KV_INT8 && C::is_nan(kfirst)) kscale = NAN;
       const unsigned vbads = (unsigned)__ballot(vbad);
-      if (kScaleOnLogits && C::is_nan(kw[0][0])) kscale = NAN;
-      if (hf == 0) {
-        vsf[n] = vscale;
-        if (kScaleOnLogits) ksf[n] = kscale;
-      }
+      if (hf == 0) vsf[key] = vscale, ksf[key] = kscale;
 
-      // S^T = K Q^T; accumulator e is key 8 (e / 4) + 4 hf + e % 4
-      f32x16 s;
+      // S^T = K Q^T; accumulator r of tile t is key 16 t + 4 kg + r
+      f32x4 s[kTiles][2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+      for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j)
+        for (int j = 0; j < kTiles; ++j) s[j][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const u32x4 f = {to_bf16<FORMAT>(kw[j][2 * z], 0, kscale), to_bf16<FORMAT>(kw[j][2 * z], 1, kscale),
-                           to_bf16<FORMAT>(kw[j][2 * z + 1], 0, kscale), to_bf16<FORMAT>(kw[j][2 * z + 1], 1, kscale)};
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), qf[2 * j + z], s, 0, 0, 0);
+        for (int c = 0; c < kFrags; ++c) {
+          const unsigned w0 = kw[t][c / 2][2 * (c % 2)], w1 = kw[t][c / 2][2 * (c % 2) + 1];
+          const u32x4 f = {to_bf16<FORMAT>(w0, 0), to_bf16<FORMAT>(w0, 1), to_bf16<FORMAT>(w1, 0), to_bf16<FORMAT>(w1, 1)};
+#pragma unroll
+          for (int j = 0; j < kTiles; ++j)
+            s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), qf[j][c], s[j][t], 0, 0, 0);
         }
+      }
       if (i + 1 < nb) kept_next = keeps(i + 1);
-      if (kTerms == 3) {
+      // logits: the sum over a query's terms, which are columns n, n ^ 8 and tiles; K's scales; masked keys to -inf (after the
+      // products, so that a NaN row does not get past it)
+      float w[8];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = over_terms(s[e]);
-      }
-      if (kScaleOnLogits) {
+      for (int t = 0; t < 2; ++t) {
+        const f32x4 f = *reinterpret_cast<const f32x4 *>(ksf + 16 * t + 4 * kg);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 f = *reinterpret_cast<const f32x4 *>(ksf + 8 * g + 4 * hf);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[4 * g + e] *= f[e];
+        for (int r = 0; r < 4; ++r) {
+          float x = s[0][t][r];
+          if (kTiles == 2) {
+            x += s[kTiles - 1][t][r];
+            x += dpp_move<0x128>(x);  // row_ror 8
+          }
+          const unsigned off = unset(kept_now.w[t], 8 * r);
+          w[4 * t + r] = __uint_as_float((off & 0xFF800000u) | (~off & __float_as_uint(x * f[r])));
         }
       }
-      // masked keys to -inf (after the products, so that a NaN row does not get past it)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const unsigned off = unset(kept_now.w[e / 4], 8 * (e % 4));
-        s[e] = __uint_as_float((off & 0xFF800000u) | (~off & __float_as_uint(s[e])));
-      }
 
-      // online softmax, one head per lane pair (lane, lane ^ 32); the reference the weights are taken against
-      // only moves when the maximum has grown past it by more than 8 in log2 units
-      float mx = s[0];
+      // online softmax, a head in the four lanes that hold its column; the reference the weights are taken against only moves
+      // when the maximum has grown past it by more than 8 in log2 units
+      float mx = w[0];
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-      {
-        const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-      }
-      const float m_top = fmaxf(m_run, mx);
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, w[e]);
+      const float m_top = fmaxf(m_run, column_max(mx));
       const bool move = (m_top - m_run) * c2 > 8.0f;  // (-inf) - (-inf) is NaN: no move
       const float m_new = move ? m_top : m_run;
       const float m_ref = m_new == -INFINITY ? 0.0f : m_new;
@@ -467,58 +473,58 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
         const float corr = move ? __builtin_amdgcn_exp2f((m_run - m_ref) * c2) : 1.0f;  // old reference -inf: 0
         l_run *= corr;
 #pragma unroll
-        for (int db = 0; db < kDimBlocks; ++db)
+        for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) oacc[db][e] *= corr;
+          for (int dt = 0; dt < kDims; ++dt) {
+            f32x4 &o = oacc[j][dt];
+            o = f32x4{o[0] * corr, o[1] * corr, o[2] * corr, o[3] * corr};
+          }
       }
       m_run = m_new;
       // the weights, times the scales of V's rows; the sum is taken over the weights themselves
-      float w[16];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c2, -off));
+      for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[e], c2, -off));
+      l_run += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 #pragma unroll
-      for (int g = 0; g < 4; ++g) l_run += (w[4 * g] + w[4 * g + 1]) + (w[4 * g + 2] + w[4 * g + 3]);
+      for (int t = 0; t < 2; ++t) {
+        const f32x4 f = *reinterpret_cast<const f32x4 *>(vsf + 16 * t + 4 * kg);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 f = *reinterpret_cast<const f32x4 *>(vsf + 8 * g + 4 * hf);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[4 * g + e] *= f[e];
+        for (int r = 0; r < 4; ++r) w[4 * t + r] *= f[r];
       }
       if (vbads) {  // (wave-uniform) a weight of 0 times a NaN scale; the rows' codes
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = __uint_as_float(~unset(kept_now.w[e / 4], 8 * (e % 4)) & __float_as_uint(w[e]));
+        for (int e = 0; e < 8; ++e) w[e] = __uint_as_float(~unset(kept_now.w[e / 4], 8 * (e % 4)) & __float_as_uint(w[e]));
 #pragma unroll
-        for (int a2 = 0; a2 < 2; ++a2)
+        for (int t = 0; t < 2; ++t) {
+          // bits r of the keys in bytes r of the word
+          const unsigned gone = (((vbads >> (16 * t + 4 * kg)) & 15u) * 0x204081u & 0x01010101u) * 0xFFu;
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            // bits k of the keys in bytes k of the word
-            const unsigned gone = (((vbads >> (16 * a2 + 8 * z + 4 * hf)) & 15u) * 0x204081u & 0x01010101u) * 0xFFu;
-#pragma unroll
-            for (int db = 0; db < kDimBlocks; ++db) vw[a2][db][z] &= ~gone;
-          }
-      }
-      // this lane's term of the weights
-      unsigned p[8];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        w[e] = __builtin_fmaf(-less1, upper16(w[e]), w[e]);
-        if (kTerms == 3) w[e] = __builtin_fmaf(-less2, upper16(w[e]), w[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) p[e / 2] = __builtin_amdgcn_perm(__float_as_uint(w[e + 1]), __float_as_uint(w[e]), 0x07060302u);
-
-      // O^T += V^T P^T: accumulator e of dim block db is dim 32 db + 8 (e / 4) + 4 hf + e % 4
-#pragma unroll
-      for (int a2 = 0; a2 < 2; ++a2) {
-        const u32x4 praw = {p[4 * a2], p[4 * a2 + 1], p[4 * a2 + 2], p[4 * a2 + 3]};
-#pragma unroll
-        for (int db = 0; db < kDimBlocks; ++db) {
-          const u32x2 x = vw[a2][db];
-          const u32x4 f = {to_bf16<FORMAT>(x[0], 0, 1.0f), to_bf16<FORMAT>(x[0], 1, 1.0f), to_bf16<FORMAT>(x[1], 0, 1.0f),
-                           to_bf16<FORMAT>(x[1], 1, 1.0f)};
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, praw), oacc[db],
-                                                             0, 0, 0);
+          for (int dt = 0; dt < kDims; ++dt) vw[dt][t] &= ~gone;
         }
+      }
+      // the terms of the weights: the upper 16 bits, and in the columns from 8 on those of what remains; in the second tile
+      // those of what remains then
+      u32x4 p[kTiles];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        float r0 = __builtin_fmaf(-less, upper16(w[e]), w[e]), r1 = __builtin_fmaf(-less, upper16(w[e + 1]), w[e + 1]);
+        p[0][e / 2] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
+        if (kTiles == 2) {
+          r0 = w[e] - upper16(w[e]), r1 = w[e + 1] - upper16(w[e + 1]);
+          r0 -= upper16(r0), r1 -= upper16(r1);
+          p[kTiles - 1][e / 2] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
+        }
+      }
+
+      // O^T += V^T P^T: accumulator r of dim block dt is dim 16 dt + 4 kg + r
+#pragma unroll
+      for (int dt = 0; dt < kDims; ++dt) {
+        const unsigned x0 = vw[dt][0], x1 = vw[dt][1];
+        const u32x4 f = {to_bf16<FORMAT>(x0, 0), to_bf16<FORMAT>(x0, 1), to_bf16<FORMAT>(x1, 0), to_bf16<FORMAT>(x1, 1)};
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+          oacc[j][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, p[j]),
+                                                                oacc[j][dt], 0, 0, 0);
       }
       // every LDS read of block i has returned (the products consumed them): its slots are free for block i + 2
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -533,15 +539,17 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   // The waves' results meet in LDS, dealt out in columns as everything from here on: column c G + x is dims 4 c .. + 3 of
   // head x, 16 bytes at 16 (c G + x) of the wave's own slots, term t's share of it t kPart further; behind them the
   // head's reference (log2 units) and sum.
-  const float l_tot = l_run + __shfl_xor(l_run, 32);
-  if (head < G && term < kTerms) {
-    float4 *mine_o = reinterpret_cast<float4 *>(lds + term * S::kPart) + head;
+  float l_tot = l_run + __shfl_xor(l_run, 16);
+  l_tot += __shfl_xor(l_tot, 32);
+  if (head < G) {
 #pragma unroll
-    for (int db = 0; db < kDimBlocks; ++db)
+    for (int j = 0; j < kTiles; ++j) {
+      if (2 * j + term >= kTerms) continue;
+      float4 *mine_o = reinterpret_cast<float4 *>(lds + (2 * j + term) * S::kPart) + head;
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        mine_o[(8 * db + 2 * g + hf) * G] =
-            make_float4(oacc[db][4 * g], oacc[db][4 * g + 1], oacc[db][4 * g + 2], oacc[db][4 * g + 3]);
+      for (int dt = 0; dt < kDims; ++dt)
+        mine_o[(4 * dt + kg) * G] = make_float4(oacc[j][dt][0], oacc[j][dt][1], oacc[j][dt][2], oacc[j][dt][3]);
+    }
     if (lane < 8) reinterpret_cast<float2 *>(lds + S::kMl)[n] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * c2, l_tot);
   }
   __syncthreads();
@@ -593,8 +601,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     Merged r = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
     if (share < shares) {
       // Bound by the latency of reading the groups back: as many as there are, up to eight, are fetched at a time (one sequence
-      // at 128k, eight heads in 32 groups, four at a time 15.4 us, eight 14.6), but no more: each costs a thread three loads
-      // (plan step at batch 16 / 64k, two groups for a thread, two at a time 40.4 us, eight 41.1, sixteen 42.9).
+      // at 128k, eight heads in 28 groups, four at a time 15.4 us, eight 14.6, when all else took longer by 1 us), but no more:
+      // each costs a thread two loads (plan step at batch 16 / 64k, two groups for a thread, two at a time 40.4 us, eight
+      // 41.1, sixteen 42.9).
       const int each = (a.groups + shares - 1) / shares;
       if (each <= 2) merge_groups<2>(r, ml, po, share, shares, a.groups, col, cols, x, G);
       else if (each <= 4) merge_groups<4>(r, ml, po, share, shares, a.groups, col, cols, x, G);
@@ -671,7 +680,7 @@ struct Query<__hip_bfloat16, DAM_KV_E4M3> {  // pairs of bf16 numbers: products 
     float d = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const unsigned x = v[i / 4][i % 4], y = to_bf16<DAM_KV_E4M3>(codes[i / 2], i % 2, 1.0f);
+      const unsigned x = v[i / 4][i % 4], y = to_bf16<DAM_KV_E4M3>(codes[i / 2], i % 2);
       d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, x), __builtin_bit_cast(bf16x2, y), d, false);
     }
     return d;
@@ -891,9 +900,10 @@ int validate_grouped(const dam_decode_params *p, const void *q, const dam_quant_
 // workgroups it costs 3 to 5 us behind the loop.
 //
 // Merged lists and plans, in blocks of 32 entries: a wave per SIMD (1024) in workgroups of four as long as a wave then has no
-// more than eight blocks, which it takes at some 0.9 us each; beyond that the memory is what counts, and two waves per SIMD in
-// workgroups of eight keep more in flight (plan step at batch 16 / 64k, 13 blocks a wave: 39.7 us, with one wave per SIMD 45.0; 32
-// lists of 104 blocks: one wave per SIMD 12.9, two 13.4 to 14.1). No more workgroups than blocks need, nor than 32 a list.
+// more than eight blocks, which it takes at some 0.8 us each; beyond that the memory is what counts, and two waves per SIMD in
+// workgroups of eight keep more in flight (plan step at batch 16 / 64k, 13 blocks a wave: 38.8 us, with one wave per SIMD 45.0
+// before the last steps; 32 lists of 104 blocks: one wave per SIMD 12.2, two 13.9). No more workgroups than blocks need,
+// nor than 32 a list.
 // A list per head, in passes of 32 (d = 128) or 64 keys per wave: up to eight waves of a workgroup, and as many workgroups as
 // CUs, each with a pass at least (one sequence, 32 heads, 1600 keys: 8.5 us; 15.8 in one workgroup of 16 waves per list).
 GroupSplit splits_of(const dam_decode_params *p, int64_t max_kept, bool grouped) {
