@@ -527,8 +527,9 @@ int dam_kv_remap_lists(const dam_evict_params *params, const int32_t *window, co
  * scale byte s for K and one for V. A code c stands for c * 2^(s - 127), and for 0 where s is 0 (the library writes 0 and
  * 1 to 249). Codes: DAM_KV_E4M3, 4 exponent bits with bias 7, 3 mantissa bits, no infinities, largest value 448; DAM_KV_INT8,
  * two's complement, -127 to 127. A row that held a value that is not finite is stored as NaN throughout (e4m3 0x7F, int8
- * -128 in every place): it takes no part in the scale of its block and reads as NaN, alone among its block's rows. A row
- * whose first code is NaN is a NaN row; the library writes no others with such codes.
+ * -128 in every place): it takes no part in the scale of its block and reads as NaN, alone among its block's rows. The codes
+ * of NaN stand in every place of a row or in none: in a cache written by other means, a row with some of them may read as
+ * NaN or as numbers, for every head of its KV head.
  * Every value is a bf16 number (but for values below 2^-126, which the decodes may take as 0), so the rows read back in
  * bf16 or fp32 are the cache's values without another rounding.
  * ---------------------------------------------------------------------------------------------- */

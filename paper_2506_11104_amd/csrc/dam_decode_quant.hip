@@ -402,7 +402,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
 
       // Everything the block needs from LDS is asked for at once, for its latency to be paid once.
       const unsigned *words = reinterpret_cast<const unsigned *>(lds + S::kScales + (i & 3) * 256);
-      const unsigned kword = words[key], vword = words[32 + key], kfirst = kslot[key * D], vfirst = vslot[key * D];
+      const unsigned kword = words[key], vword = words[32 + key];
+      const int some = key * D + 4 * key % D;  // a code of the key's row (NaN throughout or nowhere), in a bank of its own
+      const unsigned kcode = kslot[some], vcode = vslot[some];
       u32x4 kw[2][D / 64];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -419,9 +421,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       // would carry them to all heads.
       float kscale = scale_value((kword >> (bits_now & 31)) & 0xFFu);
       float vscale = scale_value((vword >> (bits_now >> 8)) & 0xFFu);
-      const bool vbad = C::is_nan(vfirst);
+      const bool vbad = C::is_nan(vcode);
       if (vbad) vscale = NAN;
-      if (FORMAT == DAM_KV_INT8 && C::is_nan(kfirst)) kscale = NAN;
+      if (FORMAT == DAM_KV_INT8 && C::is_nan(kcode)) kscale = NAN;
       const unsigned vbads = (unsigned)__ballot(vbad);
       if (hf == 0) vsf[key] = vscale, ksf[key] = kscale;
 
