@@ -624,6 +624,7 @@ class QuantCache:
     vscale: torch.Tensor
     block: int
 
+
 def quant_cache(batch: int, hkv: int, capacity: int, head_dim: int, dtype=torch.float8_e4m3fn, block: int = 64,
                 device="cuda") -> QuantCache:
     """An empty cache: allocation only."""

@@ -408,3 +408,75 @@ def test_a_decode_loop_from_a_graph():
             assert torch.equal(a, b), rep
     for o, l in zip(out, lse):
         check((o, l), c, "e4m3", q, rows_kept * Bn)
+
+
+@pytest.mark.parametrize("fmt,dtype,d", [("e4m3", "bf16", 128), ("int8", "f32", 128), ("e4m3", "f32", 64)])
+def test_keys_listed_more_than_once_count_as_often(fmt, dtype, d):
+    rng = np.random.default_rng(54)
+    Bn, Hq, Hkv, cap, G = 2, 4, 2, 200, 2
+    c, q = make(54, fmt, dtype, Bn, Hq, Hkv, d, cap, 32)
+    lists = [[rng.integers(0, cap, n).astype(np.int64) for n in row] for row in ((2, 300, 65, 0), (1, 33, 500, 32))]
+    lists[0][0][:] = 7
+    check(heads(c, q, lists), c, fmt, q, lists)
+    idx, mem, ptr = [], [], [0]
+    for b in range(Bn):
+        for h in range(Hkv):
+            for x in range(G):
+                idx.append(lists[b][h * G + x]), mem.append(np.full(len(idx[-1]), 1 << x))
+            ptr.append(sum(len(x) for x in idx))
+    got = B.dam_sparse_attn_decode_grouped_quantized(q, c, i32(ptr), i32(np.concatenate(idx)), u8(np.concatenate(mem)),
+                                                     int(np.diff(ptr).max()), want_lse=True)
+    check(got, c, fmt, q, lists)
+
+
+@pytest.mark.parametrize("fmt,dtype,d", [("e4m3", "bf16", 128), ("int8", "f32", 64)])
+def test_a_cache_of_one_row_and_blocks_larger_than_the_cache(fmt, dtype, d):
+    for cap, block in ((1, 16), (1, 128), (17, 128), (33, 32)):
+        c, q = make(55, fmt, dtype, 1, 3, 1, d, cap, block)
+        lists = [[np.arange(cap), np.arange(0), np.arange(cap - 1, cap)]]
+        for f in (heads, merged):
+            check(f(c, q, lists), c, fmt, q, lists)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("fmt,dtype,d", [("e4m3", "bf16", 128), ("int8", "f32", 128), ("e4m3", "f32", 64), ("int8", "bf16", 64)])
+def test_a_query_that_is_not_finite_stays_alone(fmt, dtype, d, value):
+    rng = np.random.default_rng(56)
+    Bn, Hq, Hkv, cap = 1, 6, 2, 900
+    c, q = make(56, fmt, dtype, Bn, Hq, Hkv, d, cap, 64)
+    lists = [pick(rng, cap, [500, 40, 300, 900, 31, 200])]
+    bad = q.clone()
+    bad[0, 1, 5] = value
+    rest = [0, 2, 3, 4, 5]
+    for f in (heads, merged):
+        want, want_lse = f(c, q, lists)
+        got, lse = f(c, bad, lists)
+        torch.cuda.synchronize()
+        assert torch.equal(got[:, rest], want[:, rest]) and torch.equal(lse[:, rest], want_lse[:, rest])
+        assert torch.isnan(got[0, 1]).all()
+
+
+def test_two_calls_at_once():
+    """On two streams, each with a workspace of its own, many times over: the results of the calls alone."""
+    rng = np.random.default_rng(57)
+    cap = 6000
+    c, _ = make(57, "e4m3", "bf16", 2, 8, 2, 128, cap, 64)
+    qs = [torch.randn((2, 8, 128), generator=torch.Generator().manual_seed(s)).to(torch.bfloat16).cuda() for s in (58, 59)]
+    lists = [[pick(rng, cap, rng.integers(1000, 3000, 8)) for _ in range(2)] for _ in qs]
+    calls = []
+    for q, ls in zip(qs, lists):
+        ptr, idx, mem = oracle.group_lists([x for b in ls for x in b], 4)
+        most = int(np.diff(ptr).max())
+        calls.append((q, c, i32(ptr), i32(idx), u8(mem), most))
+    ws = [B.decode_quantized_workspace(q, c, a[5], True) for q, a in zip(qs, calls)]
+    outs = [torch.empty((20, *q.shape), dtype=q.dtype, device="cuda") for q in qs]
+    want = [B.dam_sparse_attn_decode_grouped_quantized(*a, ws=w).clone() for a, w in zip(calls, ws)]
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, a, w, o in zip(streams, calls, ws, outs):
+            with torch.cuda.stream(s):
+                B.dam_sparse_attn_decode_grouped_quantized(*a, ws=w, out=o[i])
+    torch.cuda.synchronize()
+    for o, x in zip(outs, want):
+        assert all(torch.equal(y, x) for y in o)
