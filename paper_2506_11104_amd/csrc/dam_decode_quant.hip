@@ -63,7 +63,7 @@ struct QDecodeArgs {
   int G;               // query heads per KV head
   int waves, groups;   // a list is shared by `waves` waves of each of `groups` workgroups
   int block_shift;     // log2 of the rows that share a scale
-  uint64_t flag;       // of this call (arrive_last)
+  uint64_t flag;       // of this call (Arrivals)
   float scale;
   int64_t q_sb, q_sh, kv_sb, kv_sh, kv_ss, s_sb, s_sh, o_sb, o_sh;
   int pos, n_flags;    // plans: position of the query row, length P of the pattern flags
@@ -200,6 +200,33 @@ __device__ __forceinline__ void merge_groups(Merged &r, const float *ml, const f
   }
 }
 
+// The workgroups of a list count themselves in a word of the workspace, whose content before the call is unknown: it belongs to
+// a call once its upper bits hold the call's number, and the number of workgroups that have arrived is below. The word is looked
+// at when a workgroup starts, made the call's own (where no other workgroup has) beside the partial results' stores, counted up
+// when both are done, and left as 0. So the way from a workgroup's results to the one that merges them is three trips to
+// memory (stores, count, loads), where a flag per workgroup, read back by all, takes four: one sequence at 128k, 28 workgroups a
+// list, 13.3 us instead of 14.2; at 32k 9.15 / 10.0, from a plan at 8k 8.35 / 8.9; plan step at batch 16 / 64k, two workgroups a
+// list, the same.
+constexpr uint64_t kArrived = 63;  // (more than kMostGroups)
+struct Arrivals {
+  uint64_t *word;
+  uint64_t call, seen = 0;
+  __device__ Arrivals(uint64_t *at, uint64_t flag) : word(at), call(flag & ~kArrived) {}
+  __device__ void look() { seen = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+  __device__ void claim() {
+    uint64_t was = seen;
+    if ((was & ~kArrived) != call)
+      __hip_atomic_compare_exchange_strong(word, &was, call, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  // After the workgroup's stores and its claim are done: whether it is the last of n.
+  __device__ bool last_of(int n) {
+    const uint64_t before = __hip_atomic_fetch_add(word, (uint64_t)1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((int)(before & kArrived) != n - 1) return false;
+    __hip_atomic_store(word, (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+  }
+};
+
 // A wave owns every splits-th block of 32 list entries and two LDS slots of K and V rows, filled by load-to-LDS
 // copies whose addresses come from the list; the entries are staged three blocks ahead and the scale bytes with the rows, by
 // the same kind of copy, so that every vector-memory operation of the loop is one of these copies and the waits are counted
@@ -231,6 +258,8 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   const int b = pair / a.Hkv, hkv = pair % a.Hkv;
   const int list = a.shared_lists ? hkv : pair, hq0 = hkv * G;
   const int lo = __builtin_amdgcn_readfirstlane(kept_ptr[list]), end = __builtin_amdgcn_readfirstlane(kept_ptr[list + 1]);
+  Arrivals arrivals(flags + (int64_t)pair * a.groups, a.flag);
+  if (a.groups > 1 && threadIdx.x == 0) arrivals.look();
   const int n_blocks = (end - lo + kBlk - 1) / kBlk;
   // this wave's blocks are split, split + splits, ...: every wave gets its share of each run of the list
   const int nb = n_blocks > split ? (n_blocks - split + splits - 1) / splits : 0;
@@ -538,6 +567,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     }
   }
 
+  if (a.groups > 1 && threadIdx.x == 0) arrivals.claim();
   // The waves' results meet in LDS, dealt out in columns as everything from here on: column c G + x is dims 4 c .. + 3 of
   // head x, 16 bytes at 16 (c G + x) of the wave's own slots, term t's share of it t kPart further; behind them the
   // head's reference (log2 units) and sum.
@@ -587,10 +617,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   if (a.groups == 1) return;
   stores_done();
   __syncthreads();
-  if (wave == 0) {
-    const bool is_last = arrive_last(flags + (int64_t)pair * a.groups, a.groups, group, a.flag);
-    if (lane == 0) s_last = is_last;
-  }
+  if (threadIdx.x == 0) s_last = arrivals.last_of(a.groups);
   __syncthreads();
   if (!s_last) return;
   // The last workgroup merges the groups. Threads that share a column take them in turn; where there are fewer threads than
@@ -727,6 +754,9 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
   const uint8_t *ksb = ks + b * a.s_sb + hkv * a.s_sh, *vsb = vs + b * a.s_sb + hkv * a.s_sh;
   const float sl2 = a.scale * 1.4426950408889634f;  // logits in log2 units
 
+  Arrivals arrivals(flags + (int64_t)item * a.groups, a.flag);
+  if (a.groups > 1 && threadIdx.x == 0) arrivals.look();
+
   float m = -INFINITY, l = 0.0f, o[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) o[e] = 0.0f;
@@ -786,6 +816,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
     }
   }
 
+  if (a.groups > 1 && threadIdx.x == 0) arrivals.claim();
   // the rows of a wave, to one reference; the sums over them leave four dims to every lane of sixteen
   const float M = wave_max<LPR>(m), ref = M == -INFINITY ? 0.0f : M, f = __builtin_amdgcn_exp2f(m - ref);
   l = row16_sum<LPR>(l * f);
@@ -829,10 +860,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
   if (a.groups == 1) return;
   stores_done();
   __syncthreads();
-  if (threadIdx.x < 64) {
-    const bool last = arrive_last(flags + (int64_t)item * a.groups, a.groups, group, a.flag);
-    if (threadIdx.x == 0) s_last = last;
-  }
+  if (threadIdx.x == 0) s_last = arrivals.last_of(a.groups);
   __syncthreads();
   if (!s_last) return;
   // the last workgroup: a thread per pair of dims

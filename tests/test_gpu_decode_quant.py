@@ -480,3 +480,26 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for o, x in zip(outs, want):
         assert all(torch.equal(y, x) for y in o)
+
+
+@pytest.mark.parametrize("fill", [0, 1, 0x7F, 0xFF, None])
+def test_workspaces_that_hold_anything(fill):
+    rng = np.random.default_rng(60)
+    cap = 5000
+    c, q = make(60, "e4m3", "bf16", 1, 4, 2, 128, cap, 64)
+    lists = [pick(rng, cap, [3000, 5000, 0, 4000])]
+    most = 2 * cap
+    want = [f(c, q, lists) for f in (heads, merged)]
+    for grouped, f, x in zip((False, True), (heads, merged), want):
+        ws = B.decode_quantized_workspace(q, c, most, grouped)
+        for rep in range(3):
+            if fill is None:
+                ws.copy_(torch.from_numpy(rng.integers(0, 256, ws.numel()).astype(np.uint8)))
+            else:
+                ws.fill_(fill)
+            for _ in range(2):  # and as the call left it
+                got = f(c, q, lists, ws=ws)
+                torch.cuda.synchronize()
+                assert torch.equal(got[0], x[0]) and torch.equal(got[1], x[1])
+    check(want[0], c, "e4m3", q, lists)
+    check(want[1], c, "e4m3", q, lists)
