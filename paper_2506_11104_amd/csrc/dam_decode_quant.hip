@@ -720,8 +720,11 @@ __device__ __forceinline__ void store_out(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_out(__hip_bfloat16 *p, float v) { *p = __float2bfloat16(v); }
 
 // A list per query head. A row is read by LPR adjacent lanes, and a lane keeps kUnroll keys in flight (their row numbers are
-// fetched a pass ahead); a row's scales enter once per row.
-constexpr int kUnroll = 4;
+// fetched a pass ahead); a row's scales enter once per row. Two keys a lane leave short lists more waves and workgroups to be
+// split over than four do, and long ones are held up by their arithmetic either way: one sequence with 8 fp32 heads of 1640 keys
+// 6.9 us (four: 7.9, eight: 9.4), with 32 heads of 1640 keys 7.4 (7.8, 9.6), of 6550 keys 13.0 (12.9, 13.6). Nor are there more
+// than 16 workgroups to a list, which one of them has to merge: 8 heads of 6550 keys 12.2, with up to 32 workgroups 13.7.
+constexpr int kUnroll = 2;
 constexpr int kHeadWaves = 8;
 constexpr int kMostHeadGroups = 16;
 template <typename T, int FORMAT, int D, bool WIDE>
@@ -934,8 +937,8 @@ int validate_grouped(const dam_decode_params *p, const void *q, const dam_quant_
 // workgroups of eight keep more in flight (plan step at batch 16 / 64k, 13 blocks a wave: 38.8 us, with one wave per SIMD 45.0
 // before the last steps; 32 lists of 104 blocks: one wave per SIMD 12.2, two 13.9). No more workgroups than blocks need,
 // nor than 32 a list.
-// A list per head, in passes of 32 (d = 128) or 64 keys per wave: up to eight waves of a workgroup, and as many workgroups as
-// CUs, each with a pass at least (one sequence, 32 heads, 1600 keys: 8.5 us; 15.8 in one workgroup of 16 waves per list).
+// A list per head, in passes of 16 (d = 128) or 32 keys per wave: up to eight waves of a workgroup, and as many workgroups as
+// CUs, each with a pass at least (one sequence, 32 heads, 1640 keys: 7.4 us; 15.8 in one workgroup of 16 waves per list).
 GroupSplit splits_of(const dam_decode_params *p, int64_t max_kept, bool grouped) {
   const int64_t lists = (int64_t)p->batch * (grouped ? p->hkv : p->hq);
   if (!grouped) {
