@@ -589,7 +589,8 @@ int dam_kv_dequantize(const dam_quant_params *params, const dam_quant_cache *cac
  * values are exact; with bf16 queries the softmax weights go in as two bf16 terms each (16 bits), with fp32 queries the
  * queries and the weights as three (24 bits). A NaN row makes the outputs of the heads that keep it NaN and no others. Plans
  * are decoded for every dtype and head_dim, caches of any size in every form.
- * max_kept, the lists' bounds, clamped indices and empty lists (O = 0, lse = -inf) as for those calls. */
+ * max_kept, the lists' bounds, clamped indices and empty lists (O = 0, lse = -inf) as for those calls. 2^23 query heads in all,
+ * their (sequence, KV head) pairs rounded up to eight, are too many for a launch: DAM_ERR_UNSUPPORTED. */
 size_t dam_sparse_attn_decode_quantized_workspace(const dam_decode_params *params, int64_t max_kept);
 int dam_sparse_attn_decode_quantized(const dam_decode_params *params, const void *q, const dam_quant_cache *cache,
                                      const int32_t *kept_ptr, const int32_t *kept_idx, int64_t max_kept, void *out,

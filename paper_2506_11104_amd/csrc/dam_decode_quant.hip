@@ -910,6 +910,8 @@ int validate(const dam_decode_params *p, const void *q, const dam_quant_cache *c
   if (p->dtype != DAM_F32 && p->dtype != DAM_BF16) return DAM_ERR_UNSUPPORTED;
   if (p->head_dim != 64 && p->head_dim != 128) return DAM_ERR_UNSUPPORTED;
   if (!quant_format_ok(c->format, c->block)) return DAM_ERR_UNSUPPORTED;
+  // a launch holds fewer than 2^32 threads, 512 to a list here, pairs counted in eights
+  if (((int64_t)p->batch * p->hkv + kXcd - 1) / kXcd * kXcd * (p->hq / p->hkv) >= 1 << 23) return DAM_ERR_UNSUPPORTED;
   const int per16 = p->dtype == DAM_BF16 ? 8 : 4;
   for (int i = 0; i < 2; ++i)
     if (p->q_stride[i] < 0 || p->q_stride[i] % per16 || p->o_stride[i] < 0 || c->scale_stride[i] < 0) return DAM_ERR_INVALID_ARG;

@@ -277,3 +277,18 @@ def test_replayed_from_a_graph_and_on_another_stream():
         assert torch.equal(got[0], ko) and torch.equal(got[1], vo), rep
         for x, y in ((a.k, b.k), (a.v, b.v), (a.kscale, b.kscale), (a.vscale, b.vscale)):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), rep
+
+
+def test_more_blocks_than_a_launch_has_workgroups():
+    Bn, H, d = 70001, 31, 64
+    c = B.quant_cache(Bn, H, 1, d, torch.int8, 16)
+    x = torch.randn((Bn, H, 1, d), dtype=torch.bfloat16, device="cuda")
+    B.dam_kv_quantize(c, x, -x)
+    k, v = B.dam_kv_dequantize(c, rows=1)
+    assert torch.equal(k, -v)
+    assert ((k.float() - x.float()).abs() <= x.float().abs().amax(-1, keepdim=True) / 127).all()  # half a step of at most 2 max / 127
+    few = slice(Bn - 40, Bn)
+    small = B.quant_cache(40, H, 1, d, torch.int8, 16)
+    B.dam_kv_quantize(small, x[few], -x[few])
+    for a, b in ((c.k, small.k), (c.v, small.v), (c.kscale, small.kscale), (c.vscale, small.vscale)):
+        assert torch.equal(a[few], b)

@@ -113,6 +113,12 @@ def test_grouped_decodes_refuse():
         assert decode_calls(decode(), cache(), **kw)[2] == B.DAM_ERR_INVALID_ARG
 
 
+def test_more_heads_than_a_launch_holds_are_refused():
+    for kw in (dict(batch=1 << 22), dict(batch=(1 << 31) - 1, hq=8, hkv=8), dict(batch=1 << 20, hq=8, hkv=1),
+               dict(batch=1, hq=1 << 20, hkv=1)):
+        assert set(decode_calls(decode(**kw), cache(), ws_bytes=1 << 62)) == {B.DAM_ERR_UNSUPPORTED}, kw
+
+
 def test_one_workspace_for_a_batch_that_shrinks():
     L = B.lib()
     for hq, hkv, d, dtype in ((32, 8, 128, B.DAM_BF16), (16, 16, 64, B.DAM_F32), (64, 8, 128, B.DAM_BF16), (3, 1, 64, B.DAM_BF16)):
