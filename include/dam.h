@@ -586,8 +586,8 @@ int dam_kv_dequantize(const dam_quant_params *params, const dam_quant_cache *cac
 /* dam_sparse_attn_decode, _grouped and _patterns over such a cache: the same lists, plans, parameters (dtype is that of q and
  * out, bf16 or fp32; kv_stride and kv_capacity are the cache's, its rows 16-byte aligned) and results, on the cache's values.
  * Softmax and sums are evaluated in fp32. The products of merged lists and plans run on the matrix cores, where the cache's
- * values are exact; with bf16 queries the softmax weights go in as two bf16 terms each (16 bits), with fp32 queries the
- * queries and the weights as three (24 bits). A NaN row makes the outputs of the heads that keep it NaN and no others. Plans
+ * values are exact; with bf16 queries the softmax weights go in as two bf16 terms each, off by at most 2^-17 of a weight to
+ * either side, with fp32 queries the queries and the weights as three (24 bits, all that they have). A NaN row makes the outputs of the heads that keep it NaN and no others. Plans
  * are decoded for every dtype and head_dim, caches of any size in every form.
  * max_kept, the lists' bounds, clamped indices and empty lists (O = 0, lse = -inf) as for those calls. 2^23 query heads in all,
  * their (sequence, KV head) pairs rounded up to eight, are too many for a launch: DAM_ERR_UNSUPPORTED. */

@@ -12,11 +12,13 @@
 // under its share of the memory's time (8 KB per wave at d = 128, eight waves per CU: some 4000 cycles): the codes become bf16
 // between LDS and the products, which is exact, and the scales enter per key: K's on the logits, V's on the weights.
 // A bf16 operand has 8 significant bits, and of a tile's 16 columns at most 8 hold heads. The others hold the same heads once
-// more: columns 8 t + x what the terms before t leave of head x's weights. With bf16 queries (exact as they are) two terms
-// are 16 bits, far below half a step of the output; with fp32 queries three terms are all 24 bits, in two tiles of columns, and
-// the queries themselves are split the same way, their partial logits added across the columns. (In products of 32 x 32, half
-// of whose columns were idle, a lane had twice the logits to take through the softmax: plan step at batch 16 / 64k 39.7 us,
-// now 38.8; fp32, two sequences at 32k 16.4, now 14.5; a block alone some 0.9 us, now 0.8.)
+// more: columns 8 t + x what the terms before t leave of head x's weights. With bf16 queries (exact as they are) there are two
+// terms, each rounded to nearest: a weight is off by at most 2^-17 of itself and to neither side, far below half a step of
+// the output, 2^-8. (Cut off instead of rounded, the terms were low by up to 2^-15 while the sum l took whole weights, so that
+// outputs came out low by 7e-6 in the mean.) With fp32 queries three terms, the upper 8 bits of what is left each, are
+// all 24 bits, in two tiles of columns, and the queries themselves are split the same way, their partial logits added across the
+// columns. (In products of 32 x 32, half of whose columns were idle, a lane had twice the logits to take through the softmax:
+// plan step at batch 16 / 64k 39.7 us, now 38.8; fp32, two sequences at 32k 16.4, now 14.5; a block alone some 0.9 us, now 0.8.)
 //
 // A list per query head has one column (k_decode_quant_heads): plain ALUs, a row by 4 or 8 adjacent lanes with 16 codes each.
 //
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     unsigned bits_now = copy_rows(0), bits_next = 0;
     if (nb > 1) bits_next = copy_rows(1);
 
-    const float less = term ? 1.0f : 0.0f;  // the second term of a weight: less its upper 16 bits
+    const float less = term ? 1.0f : 0.0f;  // the second term of a weight: less its first
     float *vsf = reinterpret_cast<float *>(lds + S::kFloat), *ksf = vsf + 32;
     // LDS byte offsets of this lane's operand fragments in a slot; the others differ by an XOR (and tile 1 by 16 rows). K: rows n
     // and 16 + n, quarter kg of their chunks. V: a transposing read takes eight bytes of a row per lane (lanes 2 r and 2 r + 1 of
@@ -533,14 +535,18 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
           for (int dt = 0; dt < kDims; ++dt) vw[dt][t] &= ~gone;
         }
       }
-      // the terms of the weights: the upper 16 bits, and in the columns from 8 on those of what remains; in the second tile
-      // those of what remains then
+      // the terms of the weights: in the columns below 8 the weight as bf16, from 8 on what that leaves as bf16 (fp32 queries: the
+      // upper 16 bits, those of what remains, and in the second tile of what remains then)
       u32x4 p[kTiles];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        float r0 = __builtin_fmaf(-less, upper16(w[e]), w[e]), r1 = __builtin_fmaf(-less, upper16(w[e + 1]), w[e + 1]);
-        p[0][e / 2] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
-        if (kTiles == 2) {
+        if (kTiles == 1) {
+          const unsigned first = pack_bf16(w[e], w[e + 1]);
+          p[0][e / 2] = pack_bf16(__builtin_fmaf(-less, __uint_as_float(first << 16), w[e]),
+                                  __builtin_fmaf(-less, __uint_as_float(first & 0xFFFF0000u), w[e + 1]));
+        } else {
+          float r0 = __builtin_fmaf(-less, upper16(w[e]), w[e]), r1 = __builtin_fmaf(-less, upper16(w[e + 1]), w[e + 1]);
+          p[0][e / 2] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
           r0 = w[e] - upper16(w[e]), r1 = w[e + 1] - upper16(w[e + 1]);
           r0 -= upper16(r0), r1 -= upper16(r1);
           p[kTiles - 1][e / 2] = __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u);
