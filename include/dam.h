@@ -525,7 +525,7 @@ int dam_kv_remap_lists(const dam_evict_params *params, const int32_t *window, co
  *
  * A cache holds one code of 8 bits per element, and every `block` consecutive rows of a (sequence, KV head) share one
  * scale byte s for K and one for V. A code c stands for c * 2^(s - 127), and for 0 where s is 0 (the library writes 0 and
- * 1 to 249). Codes: DAM_KV_E4M3, 4 exponent bits with bias 7, 3 mantissa bits, no infinities, largest value 448; DAM_KV_INT8,
+ * 1 to 249; a cache written by other means must not hold larger ones). Codes: DAM_KV_E4M3, 4 exponent bits with bias 7, 3 mantissa bits, no infinities, largest value 448; DAM_KV_INT8,
  * two's complement, -127 to 127. A row that held a value that is not finite is stored as NaN throughout (e4m3 0x7F, int8
  * -128 in every place): it takes no part in the scale of its block and reads as NaN, alone among its block's rows. The codes
  * of NaN stand in every place of a row or in none: in a cache written by other means, a row with some of them may read as
@@ -587,8 +587,11 @@ int dam_kv_dequantize(const dam_quant_params *params, const dam_quant_cache *cac
  * out, bf16 or fp32; kv_stride and kv_capacity are the cache's, its rows 16-byte aligned) and results, on the cache's values.
  * Softmax and sums are evaluated in fp32. The products of merged lists and plans run on the matrix cores, where the cache's
  * values are exact; with bf16 queries the softmax weights go in as two bf16 terms each, off by at most 2^-17 of a weight to
- * either side, with fp32 queries the queries and the weights as three (24 bits, all that they have). A NaN row makes the outputs of the heads that keep it NaN and no others. Plans
- * are decoded for every dtype and head_dim, caches of any size in every form.
+ * either side, with fp32 queries the queries and the weights as three (24 bits, all that they have). A NaN row makes the outputs
+ * of the heads that keep it NaN and no others. Plans are decoded for every dtype and head_dim, caches of any size in every form.
+ * V's values may have any size that the format has: sums are finite wherever the result is. A row's part is lost where its weight,
+ * relative to the largest of the head, times its scale 2^(s - 127) is below 2^-126, or below 2^-82 where the head keeps a row
+ * whose scale is 2^64 or more. Queries are multiplied by K's codes (up to 448) before K's scale enters: |q| below 2^110.
  * max_kept, the lists' bounds, clamped indices and empty lists (O = 0, lse = -inf) as for those calls. 2^23 query heads in all,
  * their (sequence, KV head) pairs rounded up to eight, are too many for a launch: DAM_ERR_UNSUPPORTED. */
 size_t dam_sparse_attn_decode_quantized_workspace(const dam_decode_params *params, int64_t max_kept);

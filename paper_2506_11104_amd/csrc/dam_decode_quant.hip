@@ -129,6 +129,31 @@ __device__ __forceinline__ u32x4 query_term(const float *p, int term) {
   return r;
 }
 
+// Weights are at most 2^8 against their reference, but V's scales reach from 2^-126 to 2^122: products and sums of the two would
+// leave fp32's range at either end. Those of a head with a kept row of a scale of 2^64 or more are therefore held 2^44 times
+// smaller (range 44), those of a head that keeps no rows but ones of scales below 2^-64 2^36 times larger (range -36); the
+// largest scale of the rows kept so far decides, and what the accumulators hold moves with it. Behind the loop the range is
+// added to the reference, in log2 units, and the sum of weights takes the factor instead: merges need not know of it, and
+// the 80 between the ends leave them 46 bits before a weight of theirs falls below 2^-126. Up to 2^31 keys the accumulators stay
+// below 2^126. Weight times scale is lost below 2^-126, in range 44 below 2^-82.
+// (The common case, no scale outside and range 0 all over the wave, is one comparison per block.)
+__device__ __forceinline__ bool in_range_0(unsigned s) { return s - 63u < 128u; }
+__device__ __forceinline__ int range_of(float scale) { return scale >= 0x1p64f ? 44 : scale < 0x1p-64f ? -36 : 0; }  // (NaN: 0)
+// Hands (m, l) on, m in log2 units, and returns the factor that O takes: a whole number in the place of m stays exact.
+__device__ __forceinline__ float hand_on_range(int range, float &m, float &l) {
+  if (range == 0 || m == -INFINITY) return 1.0f;
+  const float whole = rintf(m), f = __builtin_amdgcn_exp2f(m - whole);
+  m = whole + (float)range;
+  l = ldexpf(l * f, -range);
+  return f;
+}
+// log(2^m L)
+__device__ __forceinline__ float lse_of(float m, float L) {
+  int e;
+  const float f = frexpf(L, &e);
+  return ((m + (float)e) + log2f(f)) * 0.6931471805599453f;
+}
+
 // The largest over the four lanes that hold a column's keys.
 __device__ __forceinline__ float column_max(float x) {
   u32x2 sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -274,6 +299,8 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
     for (int dt = 0; dt < kDims; ++dt) oacc[j][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m_run = -INFINITY, l_run = 0.0f;  // reference of the weights (raw logits), this lane's part of their sum
+  int range = 0;                          // of this column's accumulators (range_of)
+  bool plain = true;                      // (wave-uniform) all are 0
 
   if (nb > 0) {
     const unsigned char *k_rows = kc + b * a.kv_sb + hkv * a.kv_sh, *v_rows = vc + b * a.kv_sb + hkv * a.kv_sh;
@@ -451,7 +478,9 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       // through the logits (K's codes do so themselves in e4m3) or the weights; a V row's codes are cleared, since the product
       // would carry them to all heads.
       float kscale = scale_value((kword >> (bits_now & 31)) & 0xFFu);
-      float vscale = scale_value((vword >> (bits_now >> 8)) & 0xFFu);
+      const unsigned vbyte = (vword >> (bits_now >> 8)) & 0xFFu;
+      float vscale = scale_value(vbyte);
+      const bool odd = __ballot(!in_range_0(vbyte)) != 0;
       const bool vbad = C::is_nan(vcode);
       if (vbad) vscale = NAN;
       if (FORMAT == DAM_KV_INT8 && C::is_nan(kcode)) kscale = NAN;
@@ -492,6 +521,29 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
         }
       }
 
+      // (wave-uniform) the range that the accumulators need with this block's kept rows
+      if (__builtin_expect(odd || !plain, 0)) {
+        float l_all = l_run + __shfl_xor(l_run, 16);
+        l_all += __shfl_xor(l_all, 32);
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!unset(kept_now.w[e / 4], 8 * (e % 4))) top = fmaxf(top, (float)range_of(vsf[16 * (e / 4) + 4 * kg + e % 4]));
+        top = column_max(top);
+        // (a head that has kept a row has a sum that is not 0: at least 2^-8 from that of the largest logit)
+        const int to = top == -INFINITY ? range : l_all == 0.0f ? (int)top : max(range, (int)top);
+        if (__ballot(to != range)) {
+#pragma unroll
+          for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+            for (int dt = 0; dt < kDims; ++dt)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) oacc[j][dt][r] = ldexpf(oacc[j][dt][r], range - to);
+        }
+        range = to;
+        plain = __ballot(range != 0) == 0;
+      }
+
       // online softmax, a head in the four lanes that hold its column; the reference the weights are taken against only moves
       // when the maximum has grown past it by more than 8 in log2 units
       float mx = w[0];
@@ -520,11 +572,14 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       l_run += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const f32x4 f = *reinterpret_cast<const f32x4 *>(vsf + 16 * t + 4 * kg);
+        f32x4 f = *reinterpret_cast<const f32x4 *>(vsf + 16 * t + 4 * kg);
+        if (__builtin_expect(!plain, 0))
+          f = f32x4{ldexpf(f[0], -range), ldexpf(f[1], -range), ldexpf(f[2], -range), ldexpf(f[3], -range)};
 #pragma unroll
         for (int r = 0; r < 4; ++r) w[4 * t + r] *= f[r];
       }
-      if (vbads) {  // (wave-uniform) a weight of 0 times a NaN scale; the rows' codes
+      // (wave-uniform) a weight of 0 times a scale that is NaN or beyond the column's range; NaN rows' codes
+      if (__builtin_expect(vbads || !plain, 0)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = __uint_as_float(~unset(kept_now.w[e / 4], 8 * (e % 4)) & __float_as_uint(w[e]));
 #pragma unroll
@@ -579,6 +634,16 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   // head's reference (log2 units) and sum.
   float l_tot = l_run + __shfl_xor(l_run, 16);
   l_tot += __shfl_xor(l_tot, 32);
+  float m_log2 = m_run == -INFINITY ? -INFINITY : m_run * c2;
+  if (__builtin_expect(!plain, 0)) {
+    const float f = hand_on_range(range, m_log2, l_tot);
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+      for (int dt = 0; dt < kDims; ++dt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) oacc[j][dt][r] *= f;
+  }
   if (head < G) {
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) {
@@ -588,14 +653,14 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
       for (int dt = 0; dt < kDims; ++dt)
         mine_o[(4 * dt + kg) * G] = make_float4(oacc[j][dt][0], oacc[j][dt][1], oacc[j][dt][2], oacc[j][dt][3]);
     }
-    if (lane < 8) reinterpret_cast<float2 *>(lds + S::kMl)[n] = make_float2(m_run == -INFINITY ? -INFINITY : m_run * c2, l_tot);
+    if (lane < 8) reinterpret_cast<float2 *>(lds + S::kMl)[n] = make_float2(m_log2, l_tot);
   }
   __syncthreads();
   const int cols = G * (D / 4);
   auto finish = [&](int x, int c, const float4 &o, float M, float L) {
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;  // (L = 0: no key; NaN stays)
     store4(out + b * a.o_sb + (int64_t)(hq0 + x) * a.o_sh + 4 * c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (lse && c == 0) lse[(int64_t)b * a.Hq + hq0 + x] = L == 0.0f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    if (lse && c == 0) lse[(int64_t)b * a.Hq + hq0 + x] = L == 0.0f ? -INFINITY : lse_of(M, L);
   };
   float4 *po = reinterpret_cast<float4 *>(part_o) + (int64_t)pair * a.groups * cols;  // [group][column]
   float *ml = part_ml + (int64_t)pair * a.groups * G * 2;                             // [group][head][2]
@@ -767,18 +832,20 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
   if (a.groups > 1 && threadIdx.x == 0) arrivals.look();
 
   float m = -INFINITY, l = 0.0f, o[16];
+  int range = 0;  // of this lane's sums (range_of)
 #pragma unroll
   for (int e = 0; e < 16; ++e) o[e] = 0.0f;
   int rows[kUnroll];
   int64_t p0 = kept_ptr[list] + ((int64_t)(group * a.waves + wave) * GROUPS + lane / LPR) * kUnroll;
   auto fetch = [&](int64_t at) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) rows[u] = at < end ? kept_idx[min(at + u, end - 1)] : 0;
+    for (int u = 0; u < kUnroll; ++u) rows[u] = kept_idx[min(at + u, end - 1)];
   };
-  fetch(p0);
+  if (p0 < end) fetch(p0);
   for (; p0 < end; p0 += stride) {
     u32x4 kf[kUnroll], vf[kUnroll];
     float kscale[kUnroll], vscale[kUnroll];
+    bool odd = range != 0;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const unsigned r = (unsigned)in_cache(rows[u], a.cap);
@@ -788,9 +855,11 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
       kf[u] = *reinterpret_cast<const u32x4 *>(kb + at);
       vf[u] = *reinterpret_cast<const u32x4 *>(vb + at);
       kscale[u] = scale_value(ksb[r >> a.block_shift]);
-      vscale[u] = scale_value(vsb[r >> a.block_shift]);
+      const unsigned vbyte = vsb[r >> a.block_shift];
+      vscale[u] = scale_value(vbyte);
+      odd |= !in_range_0(vbyte);
     }
-    if (p0 + stride < end) fetch(p0 + stride);
+    fetch(p0 + stride);  // (always, so that the waits behind it need not expect that it was not)
     float s[kUnroll], mx = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
@@ -800,13 +869,25 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
       mx = fmaxf(mx, s[u]);
     }
     // the reference of the weights moves only when the maximum has grown past it by more than 8
-    const bool move = mx > m + 8.0f;
+    const bool move = mx > m + 8.0f, none = l == 0.0f;  // (none: no row so far)
     if (__ballot(move)) {
       const float to = move ? mx : m, corr = move ? __builtin_amdgcn_exp2f(m - to) : 1.0f;
       m = to;
       l *= corr;
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[e] *= corr;
+    }
+    if (__builtin_expect(odd, 0)) {  // the range that the sums need with these rows
+      int top = range_of(vscale[0]);
+#pragma unroll
+      for (int u = 1; u < kUnroll; ++u)
+        if (p0 + u < end) top = max(top, range_of(vscale[u]));
+      const int to = none ? top : max(range, top);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] = ldexpf(o[e], range - to);
+      range = to;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) vscale[u] = ldexpf(vscale[u], -range);
     }
     const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
@@ -826,12 +907,15 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
   }
 
   if (a.groups > 1 && threadIdx.x == 0) arrivals.claim();
+  const float part = hand_on_range(range, m, l);
   // the rows of a wave, to one reference; the sums over them leave four dims to every lane of sixteen
-  const float M = wave_max<LPR>(m), ref = M == -INFINITY ? 0.0f : M, f = __builtin_amdgcn_exp2f(m - ref);
+  const float M = wave_max<LPR>(m), ref = M == -INFINITY ? 0.0f : M;
+  float f = __builtin_amdgcn_exp2f(m - ref);
   l = row16_sum<LPR>(l * f);
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
   float t[8], r[4];
+  f *= part;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const u32x2 sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[e] * f), __float_as_uint(o[e + 8] * f), false, false);
@@ -847,7 +931,7 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
   __syncthreads();
   auto finish = [&](int dim, float acc, float top, float L) {  // (L = 0: no key)
     store_out(out + b * a.o_sb + hq * a.o_sh + dim, L == 0.0f ? 0.0f : acc / L);
-    if (lse && dim == 0) lse[item] = L == 0.0f ? -INFINITY : (top + log2f(L)) * 0.6931471805599453f;
+    if (lse && dim == 0) lse[item] = L == 0.0f ? -INFINITY : lse_of(top, L);
   };
   float *po = part_o + ((int64_t)item * a.groups + group) * D, *ml = part_ml + ((int64_t)item * a.groups + group) * 2;
   for (int dim = threadIdx.x; dim < D; dim += 64 * a.waves) {
