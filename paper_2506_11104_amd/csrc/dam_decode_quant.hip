@@ -287,7 +287,8 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
   const int lo = __builtin_amdgcn_readfirstlane(kept_ptr[list]), end = __builtin_amdgcn_readfirstlane(kept_ptr[list + 1]);
   Arrivals arrivals(flags + (int64_t)pair * a.groups, a.flag);
   if (a.groups > 1 && threadIdx.x == 0) arrivals.look();
-  const int n_blocks = (end - lo + kBlk - 1) / kBlk;
+  // (entries are counted without a sign: a list may end at 2^31 - 1, and its last block a little further)
+  const int n_blocks = (int)(((unsigned)max(end - lo, 0) + kBlk - 1) / kBlk);
   // this wave's blocks are split, split + splits, ...: every wave gets its share of each run of the list
   const int nb = n_blocks > split ? (n_blocks - split + splits - 1) / splits : 0;
   const float c2 = a.scale * 1.4426950408889634f;
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     auto copy_entries = [&](int i) {
       const int e0 = entry0(i);
       const uint64_t first = (member_at + (unsigned)e0) & ~(uint64_t)3, last = (member_at + (unsigned)(end - 1)) & ~(uint64_t)3;
-      const uint64_t addr = lane < 32 ? idx_at + 4ull * (unsigned)min(e0 + key, end - 1)
+      const uint64_t addr = lane < 32 ? idx_at + 4ull * min((unsigned)e0 + (unsigned)key, (unsigned)(end - 1))
                                       : min(first + 4u * (unsigned)min(lane - 32, 8), last);
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + S::kEntries + (i & 3) * 256), addr);
     };
@@ -388,7 +389,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     const int member_shift = (int)((member_at + (unsigned)lo) & 3);  // (blocks start a multiple of 32 entries apart)
     auto keeps = [&](int i) {
       unsigned mem = lds[S::kEntries + (i & 3) * 256 + 128 + member_shift + key];
-      if (entry0(i) + key >= end) mem = 0u;
+      if ((unsigned)entry0(i) + (unsigned)key >= (unsigned)end) mem = 0u;
       if (PLAN) {
         const int v = entry(i, key);
         const bool exists = v < 0 ? a.pos + 1 + v >= 0 : v <= a.pos;
