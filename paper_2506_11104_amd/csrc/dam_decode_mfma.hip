@@ -84,7 +84,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const int b = pair / a.Hkv, hkv = pair % a.Hkv;
   const int list = a.shared_lists ? hkv : pair;
   const int lo = __builtin_amdgcn_readfirstlane(kept_ptr[list]), end = __builtin_amdgcn_readfirstlane(kept_ptr[list + 1]);
-  const int n_blocks = (end - lo + kBlk - 1) / kBlk;
+  // (entries are counted without a sign: a list may end at 2^31 - 1, and its last block a little further)
+  const int n_blocks = (int)(((unsigned)max(end - lo, 0) + kBlk - 1) / kBlk);
   // this wave's blocks are split, split + splits, ...: every wave gets its share of each run of the list
   const int nb = n_blocks > split ? (n_blocks - split + splits - 1) / splits : 0;
   const float c2 = a.scale * 1.4426950408889634f;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     auto copy_entries = [&](int i) {
       const int e0 = entry0(i);
       const uint64_t first = (member_at + (unsigned)e0) & ~(uint64_t)3, last = (member_at + (unsigned)(end - 1)) & ~(uint64_t)3;
-      const uint64_t addr = lane < 32 ? idx_at + 4ull * (unsigned)min(e0 + lane, end - 1)
+      const uint64_t addr = lane < 32 ? idx_at + 4ull * min((unsigned)e0 + (unsigned)lane, (unsigned)(end - 1))
                                       : min(first + 4u * (unsigned)min(lane - 32, 8), last);
       lds_copy4_at(__builtin_amdgcn_readfirstlane(lds_base + kEntries + (i & 3) * 256), addr);
     };
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       // which heads keep which key: lane k < 32 holds the member byte of key k of the block
       const int e0 = entry0(i);
       const int shift = (int)((member_at + (unsigned)e0) & 3);
-      unsigned mem = lane < 32 && e0 + lane < end ? entries[128 + shift + lane] : 0u;
+      unsigned mem = lane < 32 && (unsigned)e0 + (unsigned)lane < (unsigned)end ? entries[128 + shift + lane] : 0u;
       if (PLAN) {
         const int v = *reinterpret_cast<const int *>(entries + 4 * (lane & 31));
         const bool exists = v < 0 ? a.pos + 1 + v >= 0 : v <= a.pos;

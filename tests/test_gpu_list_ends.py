@@ -48,7 +48,7 @@ def decodes(form):
     return f
 
 
-FORMS = ["merged, 8 bits", "plan, 8 bits"]
+FORMS = ["merged", "plan", "merged, 8 bits", "plan, 8 bits"]
 
 
 @pytest.mark.parametrize("form", FORMS)
