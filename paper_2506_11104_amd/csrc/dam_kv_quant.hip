@@ -15,6 +15,7 @@
 #include "dam_internal.h"
 #include "dam_mfma.h"
 #include "dam_quant.h"
+#include "dam_span.h"
 
 namespace {
 using namespace dam;
@@ -27,17 +28,10 @@ struct QuantArgs {
   int64_t c_sb, c_sh, c_ss, s_sb, s_sh;
 };
 
-// Where the rows of sequence b go. (The arrays are device data that the host cannot check: a start outside the cache has
-// no rows, and none are taken beyond the cache's end or the caller's rows.)
-struct Span {
-  int start, count;
-  __device__ Span(const QuantArgs &a, int b, const int *start_at, const int *count_at) {
-    start = start_at ? start_at[b] : a.pos;
-    count = count_at ? min(max(count_at[b], 0), a.n_rows) : a.n_rows;
-    if (start < 0 || start >= a.cap) start = 0, count = 0;
-    count = min(count, a.cap - start);
-  }
-};
+// Where the rows of sequence b go.
+__device__ __forceinline__ Span span_of(const QuantArgs &a, int b, const int *start_at, const int *count_at) {
+  return dam::span_of(start_at ? start_at[b] : a.pos, count_at ? count_at[b] : a.n_rows, a.n_rows, a.cap);
+}
 
 // Eight elements of a row as read, their largest magnitude (fp32 bits) and their codes.
 template <typename T>
@@ -148,9 +142,10 @@ __global__ __launch_bounds__(256) void k_kv_quantize(QuantArgs a, const T *__res
     const int nth = (int)(unit % a.n_blocks);
     const int64_t rest = unit / a.n_blocks;
     const int h = (int)(rest % a.Hkv), is_v = (int)(rest / a.Hkv % 2), b = (int)(rest / a.Hkv / 2);
-    const Span span(a, b, start_at, count_at);
-    const int block = span.start / BLK + nth, first = block * BLK;  // first row of the block
-    if (first >= span.start + span.count) continue;                 // (the whole workgroup)
+    const Span span = span_of(a, b, start_at, count_at);
+    const int block = nth_block(span, BLK, nth);
+    if (block < 0) continue;        // (the whole workgroup)
+    const int first = block * BLK;  // first row of the block
     const T *x = (is_v ? v : k) + b * a.x_sb[is_v] + h * a.x_sh[is_v] + lane8;
     uint8_t *codes = (is_v ? vcache : kcache) + b * a.c_sb + h * a.c_sh + first * a.c_ss + lane8;
     uint8_t *scale = (is_v ? vscale : kscale) + b * a.s_sb + h * a.s_sh + block;
@@ -213,7 +208,7 @@ __global__ __launch_bounds__(256) void k_kv_dequantize(QuantArgs a, int shift, c
     const int nth = (int)(unit % a.n_blocks);
     const int64_t rest = unit / a.n_blocks;
     const int h = (int)(rest % a.Hkv), is_v = (int)(rest / a.Hkv % 2), b = (int)(rest / a.Hkv / 2);
-    const Span span(a, b, start_at, count_at);
+    const Span span = span_of(a, b, start_at, count_at);
     const uint8_t *codes = (is_v ? vcache : kcache) + b * a.c_sb + h * a.c_sh + lane8;
     const uint8_t *scale = (is_v ? vscale : kscale) + b * a.s_sb + h * a.s_sh;
     T *x = (is_v ? v : k) + b * a.x_sb[is_v] + h * a.x_sh[is_v] + lane8;
@@ -242,7 +237,7 @@ __global__ __launch_bounds__(256) void k_kv_dequantize(QuantArgs a, int shift, c
   }
 }
 
-constexpr int kMostRows = INT32_MAX - 1024;  // row numbers of whole blocks stay within 32 bits
+constexpr int kMostRows = INT32_MAX - 1024;  // row numbers within a block that holds a row stay within 32 bits
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -323,10 +318,7 @@ extern "C" int dam_kv_quantize(const dam_quant_params *p, const dam_quant_cache 
   if (bad != DAM_OK) return bad;
   if (!start && !count && p->n_rows > p->kv_capacity - p->pos) return DAM_ERR_INVALID_ARG;
   if (p->n_rows == 0) return DAM_OK;
-  // blocks that n rows touch where they start in a block's last row, and no more than the cache has
-  const int64_t n_blocks = std::min<int64_t>(((int64_t)p->n_rows + cache->block - 2) / cache->block + 1,
-                                             ((int64_t)p->kv_capacity + cache->block - 1) / cache->block);
-  const QuantArgs a = make_args(p, cache, n_blocks);
+  const QuantArgs a = make_args(p, cache, most_blocks(p->n_rows, p->kv_capacity, cache->block));
   hipStream_t st = static_cast<hipStream_t>(stream_v);
   const bool e4m3 = cache->format == DAM_KV_E4M3, wide = p->head_dim == 128;
   if (p->dtype == DAM_BF16) {
