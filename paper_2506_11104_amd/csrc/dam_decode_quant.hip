@@ -65,6 +65,7 @@ struct QDecodeArgs {
   int G;               // query heads per KV head
   int waves, groups;   // a list is shared by `waves` waves of each of `groups` workgroups
   int block_shift;     // log2 of the rows that share a scale
+  int by_xcd;          // lists per head: a (sequence, KV head) pair has an XCD of its own
   uint64_t flag;       // of this call (Arrivals)
   float scale;
   int64_t q_sb, q_sh, kv_sb, kv_sh, kv_ss, s_sb, s_sh, o_sb, o_sh;
@@ -811,10 +812,10 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
   __shared__ float2 s_ml[kHeadWaves];
   __shared__ int s_last;
 
-  // block n runs on XCD n % 8: all workgroups of a (sequence, KV head) pair have ids with the same n % 8, so that its heads
-  // find the rows they share in one L2
-  const int per_pair = a.G * a.groups, slot = (int)blockIdx.x / kXcd;
-  const int pair = slot / per_pair * kXcd + (int)blockIdx.x % kXcd;
+  // block n runs on XCD n % 8. by_xcd: all workgroups of a (sequence, KV head) pair have ids with the same n % 8, so that its
+  // heads find the rows they share in one L2; else they are dealt out over the XCDs in turn
+  const int per_pair = a.G * a.groups, slot = (int)blockIdx.x / (a.by_xcd ? kXcd : 1);
+  const int pair = a.by_xcd ? slot / per_pair * kXcd + (int)blockIdx.x % kXcd : slot / per_pair;
   if (pair >= a.B * a.Hkv) return;
   const int b = pair / a.Hkv, hkv = pair % a.Hkv;
   const int hq = hkv * a.G + slot % per_pair / a.groups, group = slot % a.groups, item = b * a.Hq + hq;
@@ -1053,6 +1054,12 @@ GroupSplit splits_of(const dam_decode_params *p, int64_t max_kept, bool grouped)
   return {per, (int)std::min<int64_t>({(w + per - 1) / per, 256 / lists, (int64_t)kMostGroups})};
 }
 
+// Lists per head: whether a (sequence, KV head) pair has an XCD of its own, whose L2 its heads' common rows go to. Where the pairs
+// leave an XCD a quarter more work than its share, or whole XCDs idle, the workgroups are dealt out over all of them instead.
+// Own XCD / dealt out: 8 pairs of 4 heads 7.4 / 8.0 us, 14 pairs 8.2 / 8.4, 20 pairs of 8 heads 11.5 / 12.6; 12 pairs 8.9 / 8.3, 18 pairs
+// 10.2 / 9.1, 9 pairs of 8 heads 10.6 / 8.7, 4 pairs 8.9 / 7.6, 2 pairs of 4 heads 8.1 / 7.2, one pair of 8 heads of 3000 keys 12.4 / 7.9.
+bool pair_by_xcd(int64_t pairs) { return (pairs + kXcd - 1) / kXcd * kXcd * 4 <= pairs * 5; }
+
 // What a call writes to its workspace; lists of query heads, or of KV heads.
 Partials partials(void *ws, const dam_decode_params *p, int64_t max_kept, bool grouped) {
   return Partials(ws, p, splits_of(p, max_kept, grouped).groups, (int64_t)p->batch * (grouped ? p->hkv : p->hq));
@@ -1098,7 +1105,8 @@ int launch_group(const Call &x, const QDecodeArgs &a, const Partials &part) {
 
 template <typename T, int FORMAT, int D, bool WIDE>
 int launch_heads(const Call &x, const QDecodeArgs &a, const Partials &part) {
-  k_decode_quant_heads<T, FORMAT, D, WIDE><<<(a.B * a.Hkv + kXcd - 1) / kXcd * kXcd * a.G * a.groups, 64 * a.waves, 0, x.st>>>(
+  const int pairs = a.by_xcd ? (a.B * a.Hkv + kXcd - 1) / kXcd * kXcd : a.B * a.Hkv;
+  k_decode_quant_heads<T, FORMAT, D, WIDE><<<pairs * a.G * a.groups, 64 * a.waves, 0, x.st>>>(
       a, static_cast<const T *>(x.q), static_cast<const uint8_t *>(x.c->kcache), static_cast<const uint8_t *>(x.c->vcache),
       x.c->kscale, x.c->vscale, x.kept_ptr, x.kept_idx, part.o, part.ml, part.flags, static_cast<T *>(x.out), x.lse);
   return launch_status();
@@ -1131,6 +1139,7 @@ int run(const Call &x, int64_t max_kept, void *ws) {
   const GroupSplit split = splits_of(p, max_kept, x.grouped);
   a.waves = split.waves; a.groups = split.groups;
   a.block_shift = x.c->block == 16 ? 4 : x.c->block == 32 ? 5 : x.c->block == 64 ? 6 : 7;
+  a.by_xcd = pair_by_xcd((int64_t)p->batch * p->hkv);
   a.flag = a.groups > 1 ? fresh_flag() : 0;
   a.scale = p->scale > 0.0f ? p->scale : 1.0f / sqrtf((float)p->head_dim);
   a.q_sb = p->q_stride[0]; a.q_sh = p->q_stride[1];
