@@ -87,9 +87,6 @@ struct Frag<__hip_bfloat16> {
   }
 };
 
-__device__ __forceinline__ void store_out(float *p, float v) { *p = v; }
-__device__ __forceinline__ void store_out(__hip_bfloat16 *p, float v) { *p = __float2bfloat16(v); }
-
 // The end of a split: acc (of dim threadIdx.x < D), M and Lsum are the workgroup's result for one query head. A single
 // split normalises and stores it; otherwise it goes to the workspace.
 template <typename T, int D>

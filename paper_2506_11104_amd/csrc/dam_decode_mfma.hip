@@ -46,11 +46,6 @@ struct MfmaArgs {
   int pos, n_flags;    // PLAN: position of the query row, length P of the pattern flags
 };
 
-// Four bytes per lane from a 64-bit address of the lane's own to LDS address lds_at + 4 * lane.
-__device__ __forceinline__ void lds_copy4_at(unsigned lds_at, uint64_t addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_at), "v"(addr) : "memory", "m0");
-}
-
 // (The register budget of two waves per SIMD, although LDS admits one: with all 512 registers on offer the
 // compiler keeps the O accumulators in the accumulation registers for the products and in vector registers for
 // the occasional rescaling, and moves all 64 of them both ways in every iteration.)

@@ -72,10 +72,7 @@ struct QDecodeArgs {
   int pos, n_flags;    // plans: position of the query row, length P of the pattern flags
 };
 
-// Four or sixteen bytes per lane from a 64-bit address of the lane's own to LDS address lds_at (+ IMM) + 4 or 16 * lane.
-__device__ __forceinline__ void lds_copy4_at(unsigned lds_at, uint64_t addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_at), "v"(addr) : "memory", "m0");
-}
+// Sixteen bytes per lane from a 64-bit address of the lane's own to LDS address lds_at + IMM + 16 * lane.
 template <int IMM>
 __device__ __forceinline__ void lds_copy16_at(unsigned lds_at, uint64_t addr) {
   asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off"
@@ -789,9 +786,6 @@ struct Query<__hip_bfloat16, DAM_KV_E4M3> {  // pairs of bf16 numbers: products 
   }
 };
 
-__device__ __forceinline__ void store_out(float *p, float v) { *p = v; }
-__device__ __forceinline__ void store_out(__hip_bfloat16 *p, float v) { *p = __float2bfloat16(v); }
-
 // A list per query head. A row is read by LPR adjacent lanes, and a lane keeps kUnroll keys in flight (their row numbers are
 // fetched a pass ahead); a row's scales enter once per row. Two keys a lane leave short lists more waves and workgroups to be
 // split over than four do, and long ones are held up by their arithmetic either way: one sequence with 8 fp32 heads of 1640 keys
@@ -991,8 +985,6 @@ __global__ __launch_bounds__(64 * kHeadWaves) void k_decode_quant_heads(
     finish(2 * at + 1, acc.y, top, L);
   }
 }
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 int validate(const dam_decode_params *p, const void *q, const dam_quant_cache *c, const int32_t *kept_ptr,
              const int32_t *kept_idx, int64_t max_kept, const void *out) {

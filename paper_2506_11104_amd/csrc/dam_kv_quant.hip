@@ -239,8 +239,6 @@ __global__ __launch_bounds__(256) void k_kv_dequantize(QuantArgs a, int shift, c
 
 constexpr int kMostRows = INT32_MAX - 1024;  // row numbers within a block that holds a row stay within 32 bits
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
 // `write`: the caches and scales are written, else k and v are.
 int validate(const dam_quant_params *p, const dam_quant_cache *c, const void *k, const void *v, bool write) {
   if (!p || !c || (p->n_rows != 0 && (!k || !v)) || !c->kcache || !c->vcache || !c->kscale || !c->vscale) return DAM_ERR_INVALID_ARG;

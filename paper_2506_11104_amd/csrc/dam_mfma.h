@@ -58,6 +58,11 @@ __device__ __forceinline__ void lds_copy4(unsigned lds_at, const void *gbase, un
                : "memory", "scc", "m0");
 }
 
+// Four bytes per lane from a 64-bit address of the lane's own to LDS address lds_at + 4 * lane.
+__device__ __forceinline__ void lds_copy4_at(unsigned lds_at, uint64_t addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_at), "v"(addr) : "memory", "m0");
+}
+
 // 0 or -inf for bit POS of `inv` clear or set
 template <int POS>
 __device__ __forceinline__ float neg_inf_if_bit(int inv) {

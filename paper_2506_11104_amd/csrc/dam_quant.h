@@ -17,6 +17,8 @@ inline bool quant_format_ok(int format, int block) {
   return (format == DAM_KV_E4M3 || format == DAM_KV_INT8) && (block == 16 || block == 32 || block == 64 || block == 128);
 }
 
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
 #ifdef __HIPCC__
 // 2^(s - 127) for s from 1 to 254, 0 for s = 0
 __device__ __forceinline__ float scale_value(unsigned s) { return __uint_as_float(s << 23); }

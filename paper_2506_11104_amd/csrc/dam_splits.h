@@ -1,5 +1,6 @@
 // What the decodes share: sums over the lanes of a row, and the lists' splits over workgroups with the workspace they take.
 #pragma once
+#include <hip/hip_bf16.h>
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,6 +33,9 @@ __device__ __forceinline__ float row_sum(float d) {
 // fetched: there it would make the pass wait for the index load (and, the counter being in order,
 // for the rows in flight before it).
 __device__ __forceinline__ int in_cache(int row, int cap) { return min(max(row, 0), cap - 1); }
+
+__device__ __forceinline__ void store_out(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_out(__hip_bfloat16 *p, float v) { *p = __float2bfloat16(v); }
 #endif
 
 inline int pick_splits(int64_t items, int64_t max_kept) {
