@@ -228,8 +228,9 @@ __device__ __forceinline__ void merge_groups(Merged &r, const float *ml, const f
 // The workgroups of a list count themselves in a word of the workspace, whose content before the call is unknown: it belongs to
 // a call once its upper bits hold the call's number, and the number of workgroups that have arrived is below. The word is looked
 // at when a workgroup starts, made the call's own (where no other workgroup has) beside the partial results' stores, counted up
-// when both are done, and left as 0. So the way from a workgroup's results to the one that merges them is three trips to
-// memory (stores, count, loads), where a flag per workgroup, read back by all, takes four: one sequence at 128k, 28 workgroups a
+// when both are done, and left as 0. (What another call left there, or anything else, has the call's 58 upper bits with a
+// probability of 2^-58 per list.) So the way from a workgroup's results to the one that merges them is three trips to
+// memory (stores, count, loads), where a flag per workgroup, read back by all, takes four: one sequence at 128k, 27 workgroups a
 // list, 13.3 us instead of 14.2; at 32k 9.15 / 10.0, from a plan at 8k 8.35 / 8.9; plan step at batch 16 / 64k, two workgroups a
 // list, the same.
 constexpr uint64_t kArrived = 63;  // (more than kMostGroups)
@@ -700,7 +701,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     Merged r = {make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.0f};
     if (share < shares) {
       // Bound by the latency of reading the groups back: as many as there are, up to eight, are fetched at a time (one sequence
-      // at 128k, eight heads in 28 groups, four at a time 15.4 us, eight 14.6, when all else took longer by 1 us), but no more:
+      // at 128k, eight heads in 27 groups, four at a time 15.4 us, eight 14.6, when all else took longer by 1 us), but no more:
       // each costs a thread two loads (plan step at batch 16 / 64k, two groups for a thread, two at a time 40.4 us, eight
       // 41.1, sixteen 42.9).
       const int each = (a.groups + shares - 1) / shares;
