@@ -791,7 +791,8 @@ struct Query<__hip_bfloat16, DAM_KV_E4M3> {  // pairs of bf16 numbers: products 
 // fetched a pass ahead); a row's scales enter once per row. Two keys a lane leave short lists more waves and workgroups to be
 // split over than four do, and long ones are held up by their arithmetic either way: one sequence with 8 fp32 heads of 1640 keys
 // 6.9 us (four: 7.9, eight: 9.4), with 32 heads of 1640 keys 7.4 (7.8, 9.6), of 6550 keys 13.0 (12.9, 13.6). Nor are there more
-// than 16 workgroups to a list, which one of them has to merge: 8 heads of 6550 keys 12.2, with up to 32 workgroups 13.7.
+// than 16 workgroups to a list, which one of them has to merge: 8 fp32 heads of 1640 keys 7.2, with up to 32 workgroups 7.5, 8 heads
+// of 6550 keys 9.6 either way; few lists that are longer still would gain (8 heads of one KV head, 13100 keys 13.1, 11.5).
 constexpr int kUnroll = 2;
 constexpr int kHeadWaves = 8;
 constexpr int kMostHeadGroups = 16;
