@@ -401,7 +401,9 @@ size_t dam_sparse_attn_decode_workspace(const dam_decode_params *params, int64_t
  *             are device data that the host cannot check: an index outside [0, kv_capacity) is
  *             read as the nearest cache row (the output is then meaningless, no address leaves the
  *             cache); kept_ptr itself must be a valid CSR offset array.
- * lse         device f32 [batch][hq] or NULL. */
+ * lse         device f32 [batch][hq] or NULL.
+ * V's rows are summed in fp32 with weights of up to 1 (of up to 2^8 where the grouped forms below run on the matrix cores) before
+ * the division by the sum of weights: |v| summed over a head's kept keys has to stay below 2^127 (2^119). */
 int dam_sparse_attn_decode(const dam_decode_params *params, const void *q, const void *kcache,
                            const void *vcache, const int32_t *kept_ptr, const int32_t *kept_idx,
                            int64_t max_kept, void *out, float *lse, void *ws, size_t ws_bytes,
