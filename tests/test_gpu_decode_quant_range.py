@@ -118,3 +118,54 @@ def test_a_row_of_another_size_that_the_softmax_drops_or_prefers(fmt, dtype, d):
                 k[0, 0, at] = q[0, 0].float() * z * d ** 0.5 / q[0, 0].float().square().sum()
                 c = cache(g, fmt, d, block, sizes, k)
                 all_forms(c, fmt, q[:, :1].expand(1, 3, d).contiguous().cuda(), [[np.arange(cap), np.arange(0, cap, 3), np.arange(at, at + 1)]])
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_scales_of_any_size(seed):
+    """Caches whose blocks' scale bytes of V are drawn from all that the library writes, or from some of them, codes at random."""
+    rng = np.random.default_rng(8400 + seed)
+    fmt, dtype, d = FORMS[seed % len(FORMS)]
+    Bn, Hkv, G, block = int(rng.integers(1, 4)), int(rng.integers(1, 4)), int(rng.integers(1, 9)), int(rng.choice([16, 32, 64, 128]))
+    cap = int(rng.choice([1, 40, 333, 1500, 6000]))
+    c = B.quant_cache(Bn, Hkv, cap, d, DTYPE[fmt], block)
+    shape = c.kscale.shape
+    pool = (np.arange(250), np.array([0, 1, 120, 249]), np.array([1, 62, 63, 190, 191]), np.array([0, 126, 127, 128]))[seed // 4]
+    c.vscale.copy_(torch.from_numpy(rng.choice(pool, shape).astype(np.uint8)))
+    c.kscale.copy_(torch.from_numpy(rng.integers(112, 120, shape).astype(np.uint8)))
+    for x in (c.k, c.v):  # e4m3 codes up to 0x6F (120) and int8 ones up to 63: less than 2^128 with every scale
+        code = rng.integers(0, 0x70, (Bn, Hkv, cap, d)) if fmt == "e4m3" else rng.integers(-63, 64, (Bn, Hkv, cap, d))
+        if fmt == "e4m3":
+            code = code | rng.choice([0, 0x80], code.shape)
+        x.view(torch.uint8).copy_(torch.from_numpy(code.astype(np.int64).astype(np.uint8)))
+    q = torch.from_numpy(rng.standard_normal((Bn, G * Hkv, d)) * 0.1).to(T[dtype]).cuda()
+    lists = [[np.sort(rng.choice(cap, int(rng.integers(0, cap + 1)), replace=False)).astype(np.int64) for _ in range(G * Hkv)] for _ in range(Bn)]
+    for f in (heads, merged):
+        check(f(c, q, lists), c, fmt, q, lists)
+    check(planned(c, q, lists[:1]), c, fmt, q, [lists[0]] * Bn)
+
+
+@pytest.mark.parametrize("fmt,dtype,d", FORMS)
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_nan_rows_among_rows_of_every_size(fmt, dtype, d, where):
+    """A row of NaN in a block of every size: the heads that keep one are NaN, the others as without it."""
+    rng, block, cap = np.random.default_rng(85), 16, 640
+    g = torch.Generator().manual_seed(85)
+    of = np.repeat(rng.integers(0, 5, cap // block), block)
+    c = cache(g, fmt, d, block, np.array(list(SIZES.values()))[of], torch.randn((1, 1, cap, d), generator=g))
+    q = torch.randn((1, 6, d), generator=g).to(T[dtype]).cuda()
+    bad = np.array([rng.choice(np.flatnonzero(of == x)) for x in range(5)])
+    fine = np.setdiff1d(np.arange(cap), bad)
+    lists = [[fine, np.sort(np.append(fine[of[fine] == 0], bad[4])), fine[of[fine] == 0], bad[:1], fine[of[fine] >= 2], np.arange(cap)]]
+    for f in (heads, merged, planned):
+        want = f(c, q, lists)
+        x = B.QuantCache(c.k.clone(), c.v.clone(), c.kscale, c.vscale, block)
+        getattr(x, where).view(torch.uint8)[:, :, bad] = 0x7F if fmt == "e4m3" else 0x80
+        got = f(x, q, lists)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[:, [0, 2, 4]], b[:, [0, 2, 4]]) for a, b in zip(got, want))
+        assert torch.isnan(got[0][:, [1, 3, 5]]).all()
+        if where == "k":
+            assert torch.isnan(got[1][:, [1, 3, 5]]).all()
+        else:  # lse is of the logits alone. A sum may be held in another range without the row: where it is handed on an
+            # exponential and a product, 3 u, on either side, and the roundings of the reference and the logarithm, 4 u (1 + |lse|)
+            assert ((got[1] - want[1]).abs() <= 16 * U * (1 + want[1].abs())).all()
